@@ -427,6 +427,167 @@ typedef struct {
 
 pr_status pr_forest_host_image(pr_forest *f, pr_image_view *out);
 
+/*
+ * The node's KV cache: the memory whose index the local tree is (paper, System
+ * Design: updateKVCache adds a request's missing entries, evictKVCache frees
+ * an evicted token's; Algorithm 1 pairs them with updateTrie and
+ * EvictLRUTrie).  The calls below work on a paged cache in the caller's device
+ * memory, described by a pr_kv; the library keeps no state of it.
+ *
+ * A cache has num_slots sequences.  Sequence s holds lengths[s] tokens in the
+ * pages table[s][0], table[s][1], ..., page_tokens tokens each; a page may be
+ * held by several sequences (forks of a common prefix), refs counts them.
+ * Keys and values lie so that the attention's matrix instructions take them
+ * from memory without a transposition:
+ *   k  [layers][num_pages][kv_heads][head_dim / 8][page_tokens][8]
+ *   v  [layers][num_pages][kv_heads][page_tokens / 4][head_dim][4]
+ * (key dimension d of token t: block d / 8, entry d % 8; value dimension d of
+ * token t: block t / 4, entry t % 4).  The first two dimensions have strides
+ * of their own, so a page's layers may also lie together.
+ *
+ * Conventions shared by the pr_kv calls
+ *   - All pointers but the pr_kv itself are DEVICE pointers on its device.  The
+ *     calls only enqueue kernels on the stream: they neither allocate nor copy
+ *     nor wait (pr_kv_check excepted), and may be captured into a HIP graph.
+ *   - Calls that change a cache (init, extend, write, fork, trim, compact) are
+ *     ordered by the caller, as are those that read it (attend) after them: one
+ *     stream, or events.  Attends may overlap, each with its own workspace.
+ *   - Batch entries that cannot be carried out leave the cache as it was and
+ *     are counted in *skipped; see pr_kv_check.  A slot of -1 is padding: its
+ *     entry does nothing and is not counted.
+ *   - workspace: device scratch of at least pr_kv_workspace bytes, 16-byte
+ *     aligned, not read by later calls.  Calls that may overlap, or graphs that
+ *     may be replayed at the same time, need workspaces of their own.
+ *   - What pages hold behind a sequence's last token is never read as a number:
+ *     infinities and NaNs there do not reach any result.
+ */
+#define PR_KV_BF16 0
+#define PR_KV_F16 1
+#define PR_KV_E4M3 2 /* 8 bits (OCP e4m3: 448 at most, no infinities), value = stored * scale */
+
+typedef struct {
+    int32_t device;      /* HIP device of every pointer below */
+    int32_t dtype;       /* of k and v: PR_KV_BF16, PR_KV_F16 or PR_KV_E4M3 */
+    int32_t layers;      /* >= 1 */
+    int32_t kv_heads;    /* >= 1 */
+    int32_t head_dim;    /* 64, 96, 128, 192 or 256 */
+    int32_t page_tokens; /* 16, 32, 64, 128 or 256 */
+    int32_t num_pages;   /* >= 1, num_pages * page_tokens < 2^31 */
+    int32_t num_slots;   /* >= 1 */
+    int32_t slot_pages;  /* pages a sequence may have, >= 1, slot_pages * page_tokens < 2^31 */
+    float k_scale;       /* PR_KV_E4M3: finite and positive; else 1 */
+    float v_scale;
+    void *k, *v;         /* 16-byte aligned */
+    int64_t k_layer, k_page, v_layer, v_page; /* strides in elements, of a multiple of 16 bytes */
+    int32_t *table;       /* [num_slots][slot_pages], -1 past a sequence's pages */
+    int32_t *lengths;     /* [num_slots] */
+    int32_t *refs;        /* [num_pages]: sequences that hold the page */
+    uint64_t *free_pages; /* [ceil(num_pages / 64)]: bit p % 64 of word p / 64 set where refs[p] is 0 */
+    int64_t *skipped;     /* batch entries that calls left out since the last check */
+} pr_kv;
+
+/* An empty cache: every length and reference count 0, every table entry -1,
+ * every page free, nothing skipped.  k and v are left as they are.
+ * Errors, of this and every pr_kv call: PR_EINVAL (NULL or inconsistent pr_kv,
+ * NULL pointers with a non-zero count, negative counts, a workspace that is too
+ * small), PR_EDEVICE; nothing is enqueued. */
+pr_status pr_kv_init(const pr_kv *c, void *hip_stream);
+
+#define PR_KV_WORK_EXTEND 0  /* n entries, m rows */
+#define PR_KV_WORK_ATTEND 1  /* n entries, m query heads */
+#define PR_KV_WORK_COMPACT 2 /* n and m are 0 */
+
+/* Bytes (HOST, *bytes) of workspace that a call with these sizes needs. */
+pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, int64_t *bytes);
+
+/*
+ * Room for new tokens.  Entry i appends offsets[i+1] - offsets[i] tokens to
+ * sequence slots[i] (int32 [n]; offsets int64 [n + 1], non-decreasing, within
+ * [0, rows]): its length grows, it gets the pages it lacks, and
+ *   place[r]  int32 [rows]: page * page_tokens + token in the page of row r,
+ *             -1 for rows of entries that were skipped and of none.
+ * A sequence whose last page is partly filled and held by others too gets a
+ * page of its own for it, into which this call copies the filled part on every
+ * layer.  Pages are the lowest free ones, in the order of the batch; a page
+ * that the call itself frees is not among them.
+ * Skipped: a slot out of range or named by an earlier entry that appends
+ * tokens, offsets that decrease or leave [0, rows], a length past slot_pages
+ * pages, and, once the free pages do not suffice, every entry that needs one.
+ */
+pr_status pr_kv_extend(const pr_kv *c, const int32_t *slots, const int64_t *offsets, int64_t n, int64_t rows,
+                       int32_t *place, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Write keys and values of new tokens in one layer: row r (kv_heads * head_dim
+ * numbers at k_rows + r * k_stride, v_rows + r * v_stride; strides in elements)
+ * goes to place[r] (pr_kv_extend's).  io is the rows' type, PR_KV_BF16 or
+ * PR_KV_F16: the cache's own, or either for a PR_KV_E4M3 cache, which takes the
+ * nearest of its values to number / scale, ties to even, +-448 past its range,
+ * NaN for NaN.  Rows whose place is negative or past the last page are left
+ * out (not counted).
+ */
+pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const void *k_rows, int64_t k_stride,
+                      const void *v_rows, int64_t v_stride, int64_t rows, int32_t io, void *hip_stream);
+
+/*
+ * Attention of one new token a sequence over its cached tokens in one layer.
+ * Query head j of entry i (q + i * q_stride + j * head_dim) attends with the
+ * keys and values of head j / (q_heads / kv_heads) of sequence slots[i]:
+ *   s_t = scale * q . k_t,  out = sum_t exp(s_t) v_t / sum_t exp(s_t),
+ *   lse = log sum_t exp(s_t)
+ * over its tokens t, the last `window` ones if window > 0.
+ *   q    io (the cache's type; either 16-bit one for PR_KV_E4M3), 16-bit rows;
+ *   out  io [n][q_heads][head_dim];
+ *   lse  float [n][q_heads], or NULL.
+ * A sequence without tokens, padding and a slot out of range (the latter
+ * counted) give out 0 and lse -infinity.  Tokens of a page whose table entry
+ * is out of range are left out.  Sums, maxima and weights are kept in 32 bits.
+ * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
+ */
+pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int64_t n, const void *q,
+                       int64_t q_stride, int32_t q_heads, int32_t io, float scale, int32_t window, void *out,
+                       float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Reuse a cached prefix: sequence dst[i] becomes the first tokens[i] tokens of
+ * src[i], sharing their pages (int32 [n] each).  dst[i] has to be empty.  No
+ * keys or values are copied: pr_kv_extend does where a shared page is appended
+ * to.
+ * Skipped: slots out of range, tokens[i] outside [0, lengths[src[i]]], a dst
+ * that is not empty or that an earlier entry names, a src that is some entry's
+ * dst.  dst[i] -1 is padding.
+ */
+pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
+                     void *hip_stream);
+
+/*
+ * evictKVCache for a batch: sequence slots[i] keeps its first
+ * min(keep[i], length) tokens (keep NULL: none), and pages that no sequence
+ * holds any more become free.  After pr_evict_lru, the match lengths that
+ * pr_route gives for the cached sequences in the local tree are the tokens to
+ * keep.  A slot may occur more than once: the least keep holds.
+ * keep[i] is read at keep + i * keep_stride (a column of pr_route's match_len
+ * has stride num_peers).
+ * Skipped: slots out of range, negative keep.
+ */
+pr_status pr_kv_trim(const pr_kv *c, const int32_t *slots, const int32_t *keep, int64_t keep_stride, int64_t n,
+                     void *hip_stream);
+
+/*
+ * Move the held pages to the lowest ids: with L pages held, the j-th held page
+ * with an id of L or more goes to the j-th free id below L, on every layer, and
+ * the tables follow.  Afterwards pages L and up are free, and a pr_kv of L
+ * pages over the same memory (with the first entries of refs and free_pages)
+ * describes the cache.  moved (DEVICE int32 [2], or NULL): pages moved, L.
+ */
+pr_status pr_kv_compact(const pr_kv *c, int32_t *moved, void *workspace, int64_t workspace_bytes,
+                        void *hip_stream);
+
+/* Wait for the stream and report batch entries that calls skipped since the
+ * last check: PR_OK if none, else PR_EINVAL with the count in the message (and
+ * resets the count).  Not for streams under capture (PR_ESTATE). */
+pr_status pr_kv_check(const pr_kv *c, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

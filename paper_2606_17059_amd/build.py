@@ -19,7 +19,7 @@ ARCH = "gfx950"
 HIP_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-Wall", "-Wno-unused-result"]
-HIP_SOURCES = ["route", "route_team", "router"]
+HIP_SOURCES = ["route", "route_team", "router", "kvcache", "kv_attend_bf16", "kv_attend_f16"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
 
 

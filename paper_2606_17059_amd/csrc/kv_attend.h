@@ -1,0 +1,460 @@
+// kv_attend.h -- attention of one new token a sequence over the paged cache.
+//
+// out = sum_t 2^(x_t - m) v_t / sum_t 2^(x_t - m), x_t = scale log2(e) q . k_t, m
+// the largest x_t met so far: one pass over keys and values with a running
+// maximum and sum.  Nothing is read twice and a token's 4 head_dim bytes (16-bit
+// types) meet 4 * group * head_dim operations, so the pass is bound by the HBM
+// reads; the matrix units have an order of magnitude to spare.
+#ifndef PR_KV_ATTEND_H
+#define PR_KV_ATTEND_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kv_launch.h"
+#include "kv_layout.h"
+#include "wave_ops.h"
+
+namespace pr {
+
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+
+// The two 16-bit types the matrix units take.
+struct Bf16 {
+    __device__ static f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    }
+    __device__ static uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+    }
+    __device__ static float low(uint32_t p) { return __builtin_bit_cast(float, p << 16); }
+    __device__ static float high(uint32_t p) { return __builtin_bit_cast(float, p & 0xffff0000u); }
+    template <bool HI>
+    __device__ static uint32_t from_e4m3(uint32_t w) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+    }
+};
+struct F16 {
+    __device__ static f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+    }
+    __device__ static uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, f16x2{(_Float16)x, (_Float16)y});
+    }
+    __device__ static float low(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }
+    __device__ static float high(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[1]; }
+    template <bool HI>
+    __device__ static uint32_t from_e4m3(uint32_t w) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
+    }
+};
+
+// Eight numbers of the cache as they are loaded, and as the matrix units take
+// them.  An e4m3 number is a bfloat16 and a half number exactly.
+template <typename IO, bool E4M3>
+struct Eight;
+template <typename IO>
+struct Eight<IO, false> {
+    using Raw = u32x4;
+    __device__ static u32x4 wide(Raw r) { return r; }
+};
+template <typename IO>
+struct Eight<IO, true> {
+    using Raw = u32x2;
+    __device__ static u32x4 wide(Raw r) {
+        return u32x4{IO::template from_e4m3<false>(r[0]), IO::template from_e4m3<true>(r[0]),
+                     IO::template from_e4m3<false>(r[1]), IO::template from_e4m3<true>(r[1])};
+    }
+};
+
+// The larger of / the sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float rows_max(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Where a workgroup works: which entry, and which of its chunks.
+struct KvUnit {
+    int32_t entry, chunk, chunks, first_unit, chunk_tokens;
+};
+
+__device__ __forceinline__ int32_t kv_entry_length(const KvView &c, const int32_t *slots, int64_t i) {
+    const int32_t s = slots[i];
+    return kv_slot_ok(c, s) ? kv_length(c, s) : 0;
+}
+
+// Unit u of the batch's chunks in the order of its entries, found by every wave
+// for itself from the lengths (a batch of at most kKvScan entries: four a lane).
+// entry is -1 past the last unit.
+__device__ inline KvUnit kv_find_unit(const KvAttend &a, int32_t u) {
+    const int lane = (int)(threadIdx.x & 63);
+    int32_t span[kKvScan / 64];
+    int64_t total = 0;
+#pragma unroll
+    for (int e = 0; e < kKvScan / 64; ++e) {
+        const int32_t i = e * 64 + lane;
+        span[e] = i < a.n ? kv_span(kv_entry_length(a.c, a.slots, i), a.window) : 0;
+        total += span[e];
+    }
+    for (int s = 32; s; s >>= 1) total += __shfl_xor((long long)total, s);
+    KvUnit r{-1, 0, 0, 0, kv_chunk_tokens(total, a.chunks, a.least)};
+    int32_t before = 0;
+#pragma unroll
+    for (int e = 0; e < kKvScan / 64; ++e) {
+        if (e * 64 >= a.n) break;
+        const int32_t mine = e * 64 + lane < a.n ? kv_chunks(span[e], r.chunk_tokens) : 0;
+        int32_t upto = mine;
+        for (int s = 1; s < 64; s <<= 1) {
+            const int32_t o = __shfl_up(upto, s);
+            if (lane >= s) upto += o;
+        }
+        upto += before;
+        const uint64_t past = __ballot(upto > u);
+        if (past && r.entry < 0) {
+            const int src = __builtin_ctzll(past);
+            r.entry = e * 64 + src;
+            r.chunks = __builtin_amdgcn_readlane(mine, src);
+            r.first_unit = __builtin_amdgcn_readlane(upto, src) - r.chunks;
+            r.chunk = u - r.first_unit;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return r;
+}
+
+// The same from a plan (kv_plan_kernel) for larger batches: a.plan[0] is the chunk's
+// tokens, a.plan[1 + i] the units before entry i.
+__device__ inline KvUnit kv_planned_unit(const KvAttend &a, int32_t u) {
+    const int32_t *before = a.plan + 1;
+    KvUnit r{-1, 0, 0, 0, a.plan[0]};
+    if (u >= before[a.n]) return r;
+    int32_t lo = 0, hi = (int32_t)a.n;  // before[lo] <= u < before[hi]
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (before[mid] <= u) lo = mid;
+        else hi = mid;
+    }
+    r.entry = lo;
+    r.first_unit = before[lo];
+    r.chunks = before[lo + 1] - r.first_unit;
+    r.chunk = u - r.first_unit;
+    return r;
+}
+
+__global__ void __launch_bounds__(1024) kv_plan_kernel(KvAttend a);
+
+// One workgroup: one chunk of one entry's tokens, one key head, 16 R of its query
+// heads ("rows").  Its four waves take the chunk's 32-token tiles in turn, each
+// with a running maximum and sum of its own, and are joined at the end.
+//
+// Scores are taken transposed, S^T = K Q^T (16 tokens x 16 rows, head_dim / 32
+// MFMAs): a lane then holds eight of the tile's tokens of one row, which are the
+// operand's eight numbers of O^T = V^T P^T over 32 tokens, so weights never leave
+// their lane; and all of a lane's output numbers are of that row, so neither does
+// the rescaling.  Which token is which of a lane's eight is free as long as V's
+// operand agrees: a lane takes tokens 4g..4g+3 of each 16 (g = lane / 16), two
+// dimensions of four tokens being 16 contiguous bytes of a page; keys come in 16
+// contiguous bytes too.  Keys and values go from memory to the matrix units'
+// registers without LDS.
+//
+// Weights are rounded to the value's 16-bit type twice, once for the weight and
+// once for what that left over, so that the sum's terms are good to about 2^-17
+// (bf16) or 2^-22 (f16) and the output's error is its own rounding; the second
+// MFMA costs nothing next to the loads.
+template <typename IO, bool E4M3, int D, int R>
+__global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
+    using Raw = typename Eight<IO, E4M3>::Raw;
+    constexpr int KB = D / 32;  // MFMAs of a score; pairs of 16 dimensions
+    constexpr int ACC = D / 4;  // output numbers a lane holds for a row
+    constexpr int SZ = E4M3 ? 1 : 2;
+    const KvView &c = a.c;
+    const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
+    const int col = lane & 15, g = lane >> 4;
+
+    // Blocks of the same keys differ by 8, so that they share an XCD's L2.
+    const int32_t rg = (int32_t)((blockIdx.x >> 3) % (unsigned)a.row_groups);
+    const int32_t uh = (int32_t)((blockIdx.x >> 3) / (unsigned)a.row_groups * 8 + (blockIdx.x & 7));
+    const int32_t unit = uh / c.kv_heads, head = uh % c.kv_heads;
+    // without a.where every entry is one unit
+    const KvUnit w = !a.where ? KvUnit{unit < a.n ? unit : -1, 0, 1, unit, kKvMostTokens}
+                     : a.plan ? kv_planned_unit(a, unit) : kv_find_unit(a, unit);
+    if (w.entry < 0) return;
+    const int32_t entry = uniform(w.entry), chunks = uniform(w.chunks), chunk = uniform(w.chunk);
+    const int32_t slot = uniform(a.slots[entry]);
+    const bool known = kv_slot_ok(c, slot);
+    const int32_t length = known ? uniform(kv_length(c, slot)) : 0;
+    const int32_t begin = kv_first(length, a.window);
+    const int32_t from = (begin & ~(kKvTile - 1)) + chunk * w.chunk_tokens;
+    const int32_t to = (int32_t)min((int64_t)length, (int64_t)from + w.chunk_tokens);
+    if (chunk == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
+        if (a.where) {
+            a.where[2 * (int64_t)entry] = uniform(w.first_unit);
+            a.where[2 * (int64_t)entry + 1] = chunks;
+        }
+        if (!known && slot != -1) atomicAdd(c.skipped, 1ull);
+    }
+
+    const int32_t row0 = rg * 16 * R;
+    u32x4 q[R][KB];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int32_t row = row0 + 16 * r + col;
+        const bool in = row < a.group;
+        const uint16_t *src = (const uint16_t *)a.q + entry * a.q_stride + (int64_t)(head * a.group + (in ? row : 0)) * D + 8 * g;
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            u32x4 x;
+            if (a.q_aligned) {
+                x = *(const u32x4 *)(src + 32 * j);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = src[32 * j + 2 * e] | (uint32_t)src[32 * j + 2 * e + 1] << 16;
+            }
+            q[r][j] = in ? x : u32x4{0, 0, 0, 0};
+        }
+    }
+
+    f32x4 o[R][KB][2];  // dimensions 32 j + 2 (4 g + i) + e of row `col`: o[.][j][e][i]
+    float m[R], l[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < KB; ++j) o[r][j][0] = o[r][j][1] = f32x4{0, 0, 0, 0};
+    }
+
+    const int32_t *pages = c.table + (int64_t)(known ? slot : 0) * c.slot_pages;
+    const int32_t inside = kv_page_tokens(c) - 1;
+    const char *kbase = (const char *)c.k + SZ * (a.layer * c.k_layer + kv_head_base(c, head));
+    const char *vbase = (const char *)c.v + SZ * (a.layer * c.v_layer + kv_head_base(c, head));
+
+    for (int32_t t = from + kKvTile * wave; t < to; t += kKvStep) {
+        // the tile's two halves of 16 tokens, each in one page
+        int32_t pg[2];
+        bool good[2];
+        Raw kr[2][KB], vr[2][KB];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int32_t tok = t + 16 * h;
+            pg[h] = tok < to ? uniform(pages[tok >> c.page_shift]) : -1;
+            good[h] = kv_page_ok(c, pg[h]);
+            const int64_t p = good[h] ? pg[h] : 0;
+            const char *ks = kbase + SZ * (p * c.k_page + kv_key_at(c, (tok & inside) + col, 8 * g));
+            const char *vs = vbase + SZ * (p * c.v_page + kv_value_at(c, (tok & inside) + 4 * g, 2 * col));
+#pragma unroll
+            for (int j = 0; j < KB; ++j) kr[h][j] = *(const Raw *)(ks + SZ * ((int64_t)32 * j << c.page_shift));
+#pragma unroll
+            for (int j = 0; j < KB; ++j) vr[h][j] = *(const Raw *)(vs + SZ * 128 * j);
+        }
+        const bool full = good[0] && good[1] && t >= begin && t + kKvTile <= to;
+        u32x4 keep{~0u, ~0u, ~0u, ~0u};  // weights of tokens that count: two 16-bit ones a word
+        if (!full) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t tok = t + 16 * h + 4 * g + i;
+                    if (!(good[h] && tok >= begin && tok < to)) keep[2 * h + i / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
+                }
+        }
+
+        u32x4 hi[R], lo[R];
+        {
+            f32x4 s[R][2];
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < KB; ++j) {
+                    const u32x4 kk = Eight<IO, E4M3>::wide(kr[h][j]);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) s[r][h] = IO::mfma(kk, q[r][j], s[r][h]);
+                }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float x[8], top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = s[r][i >> 2][i & 3] * a.scale;
+                    if (!full && !((keep[i / 2] >> (16 * (i & 1))) & 1)) x[i] = -INFINITY;
+                    top = fmaxf(top, x[i]);
+                }
+                const float next = fmaxf(m[r], rows_max(top));
+                const float base = next == -INFINITY ? 0.f : next;  // nothing yet, or nothing but -infinity
+                const float shrink = exp2_fast(m[r] - base);
+                m[r] = next;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = exp2_fast(x[i] - base);
+                    sum += x[i];
+                }
+                l[r] = l[r] * shrink + sum;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    hi[r][i] = IO::pack(x[2 * i], x[2 * i + 1]);
+                    lo[r][i] = IO::pack(x[2 * i] - IO::low(hi[r][i]), x[2 * i + 1] - IO::high(hi[r][i]));
+                }
+                if (__ballot(!(shrink == 1.f))) {
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        o[r][j][0] *= shrink;
+                        o[r][j][1] *= shrink;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            const u32x4 v0 = Eight<IO, E4M3>::wide(vr[0][j]), v1 = Eight<IO, E4M3>::wide(vr[1][j]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                u32x4 vv{v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1]};
+                if (!full) vv &= keep;  // 0 times what lies behind a sequence could be NaN
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    o[r][j][e] = IO::mfma(vv, hi[r], o[r][j][e]);
+                    o[r][j][e] = IO::mfma(vv, lo[r], o[r][j][e]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) l[r] = rows_sum(l[r]);
+
+    // join the waves: 2 and 3 into 0 and 1, 1 into 0
+    __shared__ f32x4 so[2][R * ACC / 4][64];
+    __shared__ float sm[2][R][64], sl[2][R][64];
+#pragma unroll
+    for (int half = 2; half; half >>= 1) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                sm[wave - half][r][lane] = m[r];
+                sl[wave - half][r][lane] = l[r];
+#pragma unroll
+                for (int j = 0; j < KB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) so[wave - half][(r * KB + j) * 2 + e][lane] = o[r][j][e];
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float om = sm[wave][r][lane], next = fmaxf(m[r], om);
+                const float base = next == -INFINITY ? 0.f : next;
+                const float x = exp2_fast(m[r] - base), y = exp2_fast(om - base);
+                m[r] = next;
+                l[r] = l[r] * x + sl[wave][r][lane] * y;
+#pragma unroll
+                for (int j = 0; j < KB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        o[r][j][e] = o[r][j][e] * x + so[wave][(r * KB + j) * 2 + e][lane] * y;
+            }
+        }
+        __syncthreads();
+    }
+    if (wave) return;
+
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int32_t row = row0 + 16 * r + col;
+        if (row >= a.group) continue;
+        const int64_t at = ((int64_t)head * a.group) + row;
+        if (chunks == 1) {
+            const int64_t to_row = (int64_t)entry * a.q_heads + at;
+            if (a.lse && g == 0) a.lse[to_row] = length ? (m[r] + log2f(l[r])) * 0.6931471805599453f : -INFINITY;
+            const float unit_v = length ? c.v_scale / l[r] : 0.f;
+            uint32_t *dst = (uint32_t *)a.out + (to_row * D + 8 * g) / 2;
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                *(u32x4 *)(dst + 16 * j) =
+                    u32x4{IO::pack(o[r][j][0][0] * unit_v, o[r][j][1][0] * unit_v),
+                          IO::pack(o[r][j][0][1] * unit_v, o[r][j][1][1] * unit_v),
+                          IO::pack(o[r][j][0][2] * unit_v, o[r][j][1][2] * unit_v),
+                          IO::pack(o[r][j][0][3] * unit_v, o[r][j][1][3] * unit_v)};
+        } else {
+            const int64_t to_row = (int64_t)unit * a.q_heads + at;
+            if (g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(m[r], l[r]);
+            float *dst = a.part_o + to_row * D + 8 * g;
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                *(f32x4 *)(dst + 32 * j) = f32x4{o[r][j][0][0], o[r][j][1][0], o[r][j][0][1], o[r][j][1][1]};
+                *(f32x4 *)(dst + 32 * j + 4) = f32x4{o[r][j][0][2], o[r][j][1][2], o[r][j][0][3], o[r][j][1][3]};
+            }
+        }
+    }
+}
+
+// Joins the chunks of one entry's row: workgroup = (entry, query head), its
+// threads a group of four dimensions each, the chunks dealt to as many teams.
+template <typename IO, int D>
+__global__ void __launch_bounds__(256) kv_join_kernel(KvAttend a) {
+    constexpr int COLS = D / 4, TEAMS = 256 / COLS;
+    const int64_t entry = blockIdx.x / (unsigned)a.q_heads, row = blockIdx.x % (unsigned)a.q_heads;
+    const int32_t first = a.where[2 * entry], chunks = a.where[2 * entry + 1];
+    if (chunks <= 1) return;
+    const int cgrp = (int)threadIdx.x % COLS, team = (int)threadIdx.x / COLS;
+    __shared__ f32x4 so[TEAMS][COLS];
+    __shared__ float sml[TEAMS][2];
+    float m = -INFINITY, l = 0.f;
+    f32x4 o{0, 0, 0, 0};
+    if (team < TEAMS) {
+        for (int32_t k = team; k < chunks; k += TEAMS) {
+            const int64_t at = (int64_t)(first + k) * a.q_heads + row;
+            const float2 ml = *(const float2 *)(a.part_ml + 2 * at);
+            const f32x4 po = *(const f32x4 *)(a.part_o + at * D + 4 * cgrp);
+            const float next = fmaxf(m, ml.x), base = next == -INFINITY ? 0.f : next;
+            const float x = exp2_fast(m - base), y = exp2_fast(ml.x - base);
+            m = next;
+            l = l * x + ml.y * y;
+            o = o * x + po * y;
+        }
+        so[team][cgrp] = o;
+        if (cgrp == 0) {
+            sml[team][0] = m;
+            sml[team][1] = l;
+        }
+    }
+    __syncthreads();
+    if (team) return;
+#pragma unroll
+    for (int k = 1; k < TEAMS; ++k) {
+        const float om = sml[k][0], next = fmaxf(m, om), base = next == -INFINITY ? 0.f : next;
+        const float x = exp2_fast(m - base), y = exp2_fast(om - base);
+        m = next;
+        l = l * x + sml[k][1] * y;
+        o = o * x + so[k][cgrp] * y;
+    }
+    const int64_t to_row = entry * a.q_heads + row;
+    if (a.lse && cgrp == 0) a.lse[to_row] = (m + log2f(l)) * 0.6931471805599453f;
+    const float unit_v = a.c.v_scale / l;
+    *(u32x2 *)((uint32_t *)a.out + (to_row * D + 4 * cgrp) / 2) =
+        u32x2{IO::pack(o[0] * unit_v, o[1] * unit_v), IO::pack(o[2] * unit_v, o[3] * unit_v)};
+}
+
+}  // namespace pr
+
+#endif

@@ -1,0 +1,79 @@
+// kv_layout.h -- the paged KV cache as the kernels see it (the contract is in
+// include/prefix_router.h, pr_kv): sizes, and where numbers lie.  Plain C++, so
+// that the addresses can be walked on the CPU.
+#ifndef PR_KV_LAYOUT_H
+#define PR_KV_LAYOUT_H
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define PR_KV_FN __host__ __device__ __forceinline__
+#else
+#define PR_KV_FN inline
+#endif
+
+namespace pr {
+
+// A pr_kv without its host-side fields.
+struct KvView {
+    void *k, *v;
+    int64_t k_layer, k_page, v_layer, v_page;  // elements
+    int32_t *table, *lengths, *refs;
+    unsigned long long *free_pages;
+    unsigned long long *skipped;
+    int32_t layers, kv_heads, head_dim, page_shift, num_pages, num_slots, slot_pages;
+    float k_scale, v_scale;
+};
+
+PR_KV_FN int32_t kv_page_tokens(const KvView &c) { return 1 << c.page_shift; }
+PR_KV_FN int32_t kv_pages(const KvView &c, int64_t tokens) {
+    return (int32_t)((tokens + kv_page_tokens(c) - 1) >> c.page_shift);
+}
+PR_KV_FN bool kv_page_ok(const KvView &c, int32_t page) { return (uint32_t)page < (uint32_t)c.num_pages; }
+PR_KV_FN bool kv_slot_ok(const KvView &c, int32_t slot) { return (uint32_t)slot < (uint32_t)c.num_slots; }
+
+// Tokens a sequence holds, never more than its table row has room for.
+PR_KV_FN int32_t kv_length(const KvView &c, int32_t slot) {
+    const int32_t n = c.lengths[slot], most = c.slot_pages << c.page_shift;
+    return n < 0 ? 0 : (n < most ? n : most);
+}
+
+// Element of a page's part for one head (head_dim * page_tokens elements from
+// kv_head_base): keys lie in blocks of 8 dimensions, values in blocks of 4 tokens.
+PR_KV_FN int32_t kv_key_at(const KvView &c, int32_t token, int32_t dim) {
+    return (((dim >> 3) << c.page_shift) + token) * 8 + (dim & 7);
+}
+PR_KV_FN int32_t kv_value_at(const KvView &c, int32_t token, int32_t dim) {
+    return ((token >> 2) * c.head_dim + dim) * 4 + (token & 3);
+}
+PR_KV_FN int64_t kv_head_base(const KvView &c, int32_t head) {
+    return ((int64_t)head * c.head_dim) << c.page_shift;
+}
+
+// ---- how attention splits a batch ---------------------------------------------
+constexpr int32_t kKvMostTokens = 1 << 30;  // of a sequence
+constexpr int kKvTile = 32;        // tokens a wave takes at a time
+constexpr int kKvWaves = 4;        // waves of a workgroup
+constexpr int kKvStep = kKvTile * kKvWaves;
+
+// First token attended, rounded down to a tile, and the tiles' tokens from there.
+PR_KV_FN int32_t kv_first(int32_t length, int32_t window) {
+    return window > 0 && length > window ? length - window : 0;
+}
+PR_KV_FN int32_t kv_span(int32_t length, int32_t window) {
+    return length - (kv_first(length, window) & ~(kKvTile - 1));
+}
+
+// Tokens of a chunk: the batch's tokens over the chunks that fill the GPU, no
+// less than `least`, in whole steps of a workgroup.
+PR_KV_FN int32_t kv_chunk_tokens(int64_t tokens, int32_t chunks, int32_t least) {
+    int64_t c = (tokens + chunks - 1) / chunks;
+    c = (c + kKvStep - 1) / kKvStep * kKvStep;
+    return c < least ? least : (int32_t)c;
+}
+// Chunks of one sequence (one where it has no tokens: its output is written too).
+PR_KV_FN int32_t kv_chunks(int32_t span, int32_t chunk) { return span <= chunk ? 1 : (span + chunk - 1) / chunk; }
+
+}  // namespace pr
+
+#endif

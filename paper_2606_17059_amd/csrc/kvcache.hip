@@ -1,0 +1,387 @@
+// kvcache.hip -- the pr_kv calls of the C ABI (include/prefix_router.h): argument
+// checks and launches.  Device side: kv_pages.h, and kv_attend.h compiled in
+// kv_attend_bf16.hip and kv_attend_f16.hip.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "kv_launch.h"
+#include "kv_pages.h"
+#include "last_error.h"
+#include "prefix_router.h"
+
+namespace {
+
+using pr::KvView;
+
+pr_status fail(pr_status s, const char *msg) { return pr::set_last_error(s, msg); }
+pr_status ok() { return pr::set_last_error(PR_OK, ""); }
+
+pr_status launched(hipError_t e, const char *what) {
+    if (e == hipSuccess) return ok();
+    char msg[160];
+    snprintf(msg, sizeof msg, "%s launch failed: %s", what, hipGetErrorString(e));
+    return fail(PR_EDEVICE, msg);
+}
+
+// Makes the cache's device current for the duration of a call.
+class DeviceScope {
+   public:
+    explicit DeviceScope(int device) : device_(device) {
+        ok_ = hipGetDevice(&prev_) == hipSuccess && (prev_ == device || hipSetDevice(device) == hipSuccess);
+    }
+    ~DeviceScope() {
+        if (ok_ && prev_ != device_) (void)hipSetDevice(prev_);
+    }
+    bool ok() const { return ok_; }
+
+   private:
+    int prev_ = -1, device_;
+    bool ok_ = false;
+};
+
+constexpr int64_t kMostGrid = ((int64_t)1 << 32) / 256 - 1;  // workgroups of 256 threads in a launch
+constexpr int64_t kMostRows = INT32_MAX;
+
+int element_bytes(const pr_kv *c) { return c->dtype == PR_KV_E4M3 ? 1 : 2; }
+
+// nullptr if c describes a cache, else what is wrong with it.
+const char *wrong(const pr_kv *c) {
+    if (!c) return "pr_kv is NULL";
+    if (c->dtype != PR_KV_BF16 && c->dtype != PR_KV_F16 && c->dtype != PR_KV_E4M3) return "dtype is none of PR_KV_*";
+    if (c->device < 0) return "device is negative";
+    if (c->layers < 1 || c->kv_heads < 1 || c->num_pages < 1 || c->num_slots < 1 || c->slot_pages < 1)
+        return "layers, kv_heads, num_pages, num_slots and slot_pages must be at least 1";
+    const int d = c->head_dim, t = c->page_tokens;
+    if (d != 64 && d != 96 && d != 128 && d != 192 && d != 256) return "head_dim must be 64, 96, 128, 192 or 256";
+    if (t != 16 && t != 32 && t != 64 && t != 128 && t != 256) return "page_tokens must be 16, 32, 64, 128 or 256";
+    if ((int64_t)c->num_pages * t > INT32_MAX) return "num_pages * page_tokens must be below 2^31";
+    if ((int64_t)c->slot_pages * t > pr::kKvMostTokens) return "slot_pages * page_tokens must be at most 2^30";
+    if (!c->k || !c->v || !c->table || !c->lengths || !c->refs || !c->free_pages || !c->skipped)
+        return "pr_kv has a NULL pointer";
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return "k and v must be 16-byte aligned";
+    const int64_t unit = 16 / element_bytes(c), page = (int64_t)c->kv_heads * d * t;
+    if (c->kv_heads > (1 << 20) || page * 2 > INT32_MAX) return "a page must be smaller than 2^31 bytes";
+    for (const int64_t s : {c->k_layer, c->k_page, c->v_layer, c->v_page})
+        if (s < 0 || s % unit) return "strides must be non-negative multiples of 16 bytes";
+    if ((c->num_pages > 1 && (c->k_page < page || c->v_page < page)) ||
+        (c->layers > 1 && (c->k_layer < page || c->v_layer < page)))
+        return "pages must not overlap";
+    if (c->dtype == PR_KV_E4M3) {
+        if (!(std::isfinite(c->k_scale) && c->k_scale > 0 && std::isfinite(c->v_scale) && c->v_scale > 0))
+            return "k_scale and v_scale must be finite and positive";
+    } else if (c->k_scale != 1.f || c->v_scale != 1.f) {
+        return "k_scale and v_scale of a 16-bit cache must be 1";
+    }
+    return nullptr;
+}
+
+KvView view(const pr_kv *c) {
+    KvView v{};
+    v.k = c->k;
+    v.v = c->v;
+    v.k_layer = c->k_layer;
+    v.k_page = c->k_page;
+    v.v_layer = c->v_layer;
+    v.v_page = c->v_page;
+    v.table = c->table;
+    v.lengths = c->lengths;
+    v.refs = c->refs;
+    v.free_pages = (unsigned long long *)c->free_pages;
+    v.skipped = (unsigned long long *)c->skipped;
+    v.layers = c->layers;
+    v.kv_heads = c->kv_heads;
+    v.head_dim = c->head_dim;
+    v.page_shift = __builtin_ctz((unsigned)c->page_tokens);
+    v.num_pages = c->num_pages;
+    v.num_slots = c->num_slots;
+    v.slot_pages = c->slot_pages;
+    v.k_scale = c->k_scale;
+    v.v_scale = c->v_scale;
+    return v;
+}
+
+// Parts of a workspace, each 16-byte aligned.
+struct Parts {
+    char *base;
+    int64_t bytes = 0;
+    explicit Parts(void *p) : base((char *)p) {}
+    template <typename T>
+    T *take(int64_t count) {
+        T *p = base ? (T *)(base + bytes) : nullptr;
+        bytes += (count * (int64_t)sizeof(T) + 15) / 16 * 16;
+        return p;
+    }
+};
+
+// Room for the keys and values is at most what these rows can need, two pages an
+// entry besides whole ones, and what there is.
+int64_t pages_needed(const pr_kv *c, int64_t n, int64_t rows) {
+    return std::min<int64_t>(c->num_pages, rows / c->page_tokens + 2 * n);
+}
+
+int64_t extend_parts(const pr_kv *c, int64_t n, int64_t rows, void *work, pr::KvExtend *x) {
+    Parts p(work);
+    x->most = pages_needed(c, n, rows);
+    x->owner = p.take<int32_t>(c->num_slots);
+    x->grant = p.take<pr::KvGrant>(n);
+    x->rank = p.take<int32_t>(n);
+    x->fresh = p.take<int32_t>(x->most);
+    x->copies = p.take<int32_t>(n);
+    x->count = p.take<int32_t>(2);
+    return p.bytes;
+}
+
+int64_t compact_parts(const pr_kv *c, void *work, pr::KvCompact *x) {
+    Parts p(work);
+    x->from = p.take<int32_t>(c->num_pages / 2 + 1);
+    x->target = p.take<int32_t>(c->num_pages / 2 + 1);
+    x->to = p.take<int32_t>(c->num_pages);
+    x->count = p.take<int32_t>(2);
+    return p.bytes;
+}
+
+// How an attention is split: workgroups that fill the GPU, and the tokens that
+// are worth one.
+constexpr int kFill = 1024, kLeast = 256;
+
+// The parts of an attention's split that go by the host's numbers (a.window and
+// the cache's sizes among them), and its workspace.
+int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window, void *work, pr::KvAttend *a) {
+    const int32_t group = q_heads / c->kv_heads, rows = 16 * pr::kv_rows(group, c->head_dim);
+    a->group = group;
+    a->q_heads = q_heads;
+    a->row_groups = (group + rows - 1) / rows;
+    a->chunks = std::max(1, kFill / (c->kv_heads * a->row_groups));
+    a->least = kLeast;
+    int64_t span = (int64_t)c->slot_pages * c->page_tokens;
+    if (window > 0) span = std::min<int64_t>(span, (int64_t)window + pr::kKvTile - 1);
+    const int64_t each = (span + kLeast - 1) / kLeast, units = std::min<int64_t>(n * each, a->chunks + n);
+    a->units = (int32_t)std::min<int64_t>(units, INT32_MAX);
+    a->where = a->plan = nullptr;
+    a->part_ml = a->part_o = nullptr;
+    if (each <= 1) return 0;
+    Parts p(work);
+    a->where = p.take<int32_t>(2 * n);
+    a->plan = n > pr::kKvScan ? p.take<int32_t>(n + 2) : nullptr;
+    a->part_ml = p.take<float>(units * q_heads * 2);
+    a->part_o = p.take<float>(units * q_heads * c->head_dim);
+    return p.bytes;
+}
+
+const char *wrong_work(const void *work, int64_t have, int64_t need) {
+    if (need == 0) return nullptr;
+    if (!work || have < need) return "workspace is smaller than pr_kv_workspace says";
+    if ((uintptr_t)work & 15) return "workspace must be 16-byte aligned";
+    return nullptr;
+}
+
+const char *wrong_io(const pr_kv *c, int32_t io) {
+    if (io != PR_KV_BF16 && io != PR_KV_F16) return "io must be PR_KV_BF16 or PR_KV_F16";
+    if (c->dtype != PR_KV_E4M3 && io != c->dtype) return "io must be the type of a 16-bit cache";
+    return nullptr;
+}
+
+unsigned blocks(int64_t items, int64_t most) { return (unsigned)std::max<int64_t>(1, std::min((items + 255) / 256, most)); }
+
+}  // namespace
+
+extern "C" {
+
+pr_status pr_kv_init(const pr_kv *c, void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    const int64_t items = std::max<int64_t>((int64_t)c->num_slots * c->slot_pages, c->num_pages);
+    pr::kv_init_kernel<<<blocks(items, 2048), 256, 0, (hipStream_t)hip_stream>>>(view(c));
+    return launched(hipGetLastError(), "pr_kv_init");
+}
+
+pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, int64_t *bytes) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (!bytes) return fail(PR_EINVAL, "bytes is NULL");
+    if (n < 0 || m < 0 || n > kMostRows || m > kMostRows) return fail(PR_EINVAL, "a count is negative or past 2^31 - 1");
+    if (call == PR_KV_WORK_EXTEND) {
+        pr::KvExtend x;
+        *bytes = extend_parts(c, n, m, nullptr, &x);
+    } else if (call == PR_KV_WORK_ATTEND) {
+        if (m < 1 || m % c->kv_heads) return fail(PR_EINVAL, "q_heads must be a positive multiple of kv_heads");
+        if (n * m > kMostGrid) return fail(PR_EINVAL, "the batch has too many entries and query heads");
+        pr::KvAttend a;
+        *bytes = attend_parts(c, n, (int32_t)m, 0, nullptr, &a);
+    } else if (call == PR_KV_WORK_COMPACT) {
+        pr::KvCompact x;
+        *bytes = compact_parts(c, nullptr, &x);
+    } else {
+        return fail(PR_EINVAL, "call is none of PR_KV_WORK_*");
+    }
+    return ok();
+}
+
+pr_status pr_kv_extend(const pr_kv *c, const int32_t *slots, const int64_t *offsets, int64_t n, int64_t rows,
+                       int32_t *place, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (n < 0 || rows < 0 || n > kMostRows || rows > kMostRows)
+        return fail(PR_EINVAL, "a count is negative or past 2^31 - 1");
+    if (n == 0 && rows == 0) return ok();
+    if ((n > 0 && (!slots || !offsets)) || (rows > 0 && !place)) return fail(PR_EINVAL, "NULL device pointer");
+    pr::KvExtend x{};
+    if (const char *w = wrong_work(workspace, workspace_bytes, extend_parts(c, n, rows, workspace, &x)))
+        return fail(PR_EINVAL, w);
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    hipStream_t st = (hipStream_t)hip_stream;
+    x.c = view(c);
+    x.slots = slots;
+    x.offsets = offsets;
+    x.n = n;
+    x.rows = rows;
+    x.place = place;
+    pr::kv_extend_plan_kernel<<<1, pr::kKvPlanThreads, 0, st>>>(x);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return launched(e, "pr_kv_extend");
+    // a thread a row or new page; a wave a copied page's (layer, head, keys or values)
+    const int64_t copies = std::min<int64_t>(n * c->layers * c->kv_heads * 2, 4096) * 64;
+    const unsigned grid = blocks(std::max({rows, x.most, copies}), 65536);
+    if (c->dtype == PR_KV_E4M3) pr::kv_extend_place_kernel<uint8_t><<<grid, 256, 0, st>>>(x);
+    else pr::kv_extend_place_kernel<uint16_t><<<grid, 256, 0, st>>>(x);
+    return launched(hipGetLastError(), "pr_kv_extend");
+}
+
+pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const void *k_rows, int64_t k_stride,
+                      const void *v_rows, int64_t v_stride, int64_t rows, int32_t io, void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (layer < 0 || layer >= c->layers) return fail(PR_EINVAL, "layer out of range");
+    if (const char *w = wrong_io(c, io)) return fail(PR_EINVAL, w);
+    if (rows < 0 || rows > kMostRows) return fail(PR_EINVAL, "rows is negative or past 2^31 - 1");
+    if (rows == 0) return ok();
+    if (!place || !k_rows || !v_rows) return fail(PR_EINVAL, "NULL device pointer");
+    if (((uintptr_t)k_rows | (uintptr_t)v_rows) & 1) return fail(PR_EINVAL, "rows must be 2-byte aligned");
+    const int64_t width = (int64_t)c->kv_heads * c->head_dim;
+    if (rows > 1 && (k_stride < width || v_stride < width)) return fail(PR_EINVAL, "rows must not overlap");
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    const bool aligned = !((((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) || (rows > 1 && (k_stride | v_stride) & 7));
+    const pr::KvRows x{view(c), place, k_rows, v_rows, k_stride, v_stride, rows, layer, aligned};
+    hipStream_t st = (hipStream_t)hip_stream;
+    const unsigned grid = blocks((rows + 3) / 4 * 4 * (width / 8), kMostGrid);
+    if (c->dtype != PR_KV_E4M3) pr::kv_write_kernel<pr::KvSame><<<grid, 256, 0, st>>>(x);
+    else if (io == PR_KV_BF16) pr::kv_write_kernel<pr::KvE4m3<true>><<<grid, 256, 0, st>>>(x);
+    else pr::kv_write_kernel<pr::KvE4m3<false>><<<grid, 256, 0, st>>>(x);
+    return launched(hipGetLastError(), "pr_kv_write");
+}
+
+pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int64_t n, const void *q,
+                       int64_t q_stride, int32_t q_heads, int32_t io, float scale, int32_t window, void *out,
+                       float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (layer < 0 || layer >= c->layers) return fail(PR_EINVAL, "layer out of range");
+    if (const char *w = wrong_io(c, io)) return fail(PR_EINVAL, w);
+    if (q_heads < 1 || q_heads % c->kv_heads) return fail(PR_EINVAL, "q_heads must be a positive multiple of kv_heads");
+    if (window < 0) return fail(PR_EINVAL, "window is negative");
+    if (!std::isfinite(scale)) return fail(PR_EINVAL, "scale must be finite");
+    if (n < 0) return fail(PR_EINVAL, "n is negative");
+    if (n > kMostGrid / q_heads) return fail(PR_EINVAL, "the batch has too many entries and query heads");
+    if (n == 0) return ok();
+    if (!slots || !q || !out) return fail(PR_EINVAL, "NULL device pointer");
+    if ((uintptr_t)q & 1) return fail(PR_EINVAL, "q must be 2-byte aligned");
+    if ((uintptr_t)out & 15) return fail(PR_EINVAL, "out must be 16-byte aligned");
+    if (n > 1 && q_stride < (int64_t)q_heads * c->head_dim) return fail(PR_EINVAL, "rows of q must not overlap");
+    pr::KvAttend a{};
+    if (const char *w = wrong_work(workspace, workspace_bytes, attend_parts(c, n, q_heads, window, workspace, &a)))
+        return fail(PR_EINVAL, w);
+    a.c = view(c);
+    a.slots = slots;
+    a.n = n;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.out = out;
+    a.lse = lse;
+    a.layer = layer;
+    a.window = window;
+    a.scale = (float)((double)scale * c->k_scale * 1.4426950408889634);
+    a.q_aligned = !((uintptr_t)q & 15) && (n == 1 || !(q_stride & 7));
+    if (((int64_t)a.units * c->kv_heads + 7) / 8 * 8 * a.row_groups > kMostGrid)
+        return fail(PR_EINVAL, "the batch has too many entries and key heads");
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (a.plan) {
+        pr::kv_plan_kernel<<<1, pr::kKvPlanThreads, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return launched(e, "pr_kv_attend");
+    }
+    const bool e4m3 = c->dtype == PR_KV_E4M3;
+    return launched(io == PR_KV_BF16 ? pr::kv_launch_bf16(a, e4m3, st) : pr::kv_launch_f16(a, e4m3, st),
+                    "pr_kv_attend");
+}
+
+pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
+                     void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (n < 0 || n > kMostGrid) return fail(PR_EINVAL, "n is negative or past 2^24 - 2");
+    if (n == 0) return ok();
+    if (!src || !dst || !tokens) return fail(PR_EINVAL, "NULL device pointer");
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    pr::kv_fork_kernel<<<(unsigned)n, 256, 0, (hipStream_t)hip_stream>>>(view(c), src, dst, tokens, n);
+    return launched(hipGetLastError(), "pr_kv_fork");
+}
+
+pr_status pr_kv_trim(const pr_kv *c, const int32_t *slots, const int32_t *keep, int64_t keep_stride, int64_t n,
+                     void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    if (n < 0 || n > kMostGrid) return fail(PR_EINVAL, "n is negative or past 2^24 - 2");
+    if (keep && keep_stride < 0) return fail(PR_EINVAL, "keep_stride is negative");
+    if (n == 0) return ok();
+    if (!slots) return fail(PR_EINVAL, "NULL device pointer");
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    pr::kv_trim_kernel<<<(unsigned)n, 256, 0, (hipStream_t)hip_stream>>>(view(c), slots, keep, keep_stride);
+    return launched(hipGetLastError(), "pr_kv_trim");
+}
+
+pr_status pr_kv_compact(const pr_kv *c, int32_t *moved, void *workspace, int64_t workspace_bytes,
+                        void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    pr::KvCompact x{};
+    if (const char *w = wrong_work(workspace, workspace_bytes, compact_parts(c, workspace, &x)))
+        return fail(PR_EINVAL, w);
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    hipStream_t st = (hipStream_t)hip_stream;
+    x.c = view(c);
+    x.moved = moved;
+    pr::kv_compact_plan_kernel<<<1, pr::kKvPlanThreads, 0, st>>>(x);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return launched(e, "pr_kv_compact");
+    const int64_t items = std::max<int64_t>((int64_t)c->num_slots * c->slot_pages,
+                                            (int64_t)(c->num_pages / 2) * c->layers * 2 * 256);
+    pr::kv_compact_move_kernel<<<blocks(items, 2048), 256, 0, st>>>(x, element_bytes(c));
+    return launched(hipGetLastError(), "pr_kv_compact");
+}
+
+pr_status pr_kv_check(const pr_kv *c, void *hip_stream) {
+    if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
+    DeviceScope ds(c->device);
+    if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &cap) != hipSuccess) return fail(PR_EDEVICE, "hipStreamIsCapturing failed");
+    if (cap != hipStreamCaptureStatusNone) return fail(PR_ESTATE, "pr_kv_check waits: not under graph capture");
+    int64_t skipped = 0;
+    if (hipMemcpyAsync(&skipped, c->skipped, sizeof skipped, hipMemcpyDeviceToHost, st) != hipSuccess ||
+        hipStreamSynchronize(st) != hipSuccess)
+        return fail(PR_EDEVICE, "reading the skipped entries failed");
+    if (skipped == 0) return ok();
+    if (hipMemsetAsync(c->skipped, 0, sizeof skipped, st) != hipSuccess ||
+        hipStreamSynchronize(st) != hipSuccess)
+        return fail(PR_EDEVICE, "resetting the skipped entries failed");
+    char msg[96];
+    snprintf(msg, sizeof msg, "%lld batch entries were skipped", (long long)skipped);
+    return fail(PR_EINVAL, msg);
+}
+
+}  // extern "C"

@@ -20,6 +20,7 @@
 #include "forest_layout.h"
 #include "compact_kernels.h"
 #include "export_kernels.h"
+#include "last_error.h"
 #include "lru_kernels.h"
 #include "merge_kernels.h"
 #include "prefix_router.h"
@@ -1458,6 +1459,19 @@ struct CallScratch {
 };
 
 }  // namespace
+
+namespace pr {
+
+pr_status set_last_error(pr_status s, const char *msg) noexcept {
+    try {
+        g_err = msg;
+    } catch (...) {
+        g_err.clear();  // no memory for the message
+    }
+    return s;
+}
+
+}  // namespace pr
 
 extern "C" {
 

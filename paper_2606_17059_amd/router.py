@@ -25,7 +25,9 @@ EXPORTED = ("pr_abi_version", "pr_last_error", "pr_forest_create", "pr_forest_de
             "pr_route_noalloc",
             "pr_route_select", "pr_tree_tokens", "pr_forest_compact", "pr_set_local_peer", "pr_set_time", "pr_touch", "pr_evict_lru",
             "pr_forest_check",
-            "pr_forest_info_get", "pr_forest_host_image")
+            "pr_forest_info_get", "pr_forest_host_image",
+            "pr_kv_init", "pr_kv_workspace", "pr_kv_extend", "pr_kv_write", "pr_kv_attend", "pr_kv_fork",
+            "pr_kv_trim", "pr_kv_compact", "pr_kv_check")
 
 PR_SELECT_PREFER_LOCAL = 1
 
@@ -51,6 +53,18 @@ class ImageView(ctypes.Structure):
                 ("nodes", ctypes.POINTER(ctypes.c_int32)), ("ntok", ctypes.POINTER(ctypes.c_int32)),
                 ("nsep", ctypes.POINTER(ctypes.c_int32)), ("mext", ctypes.POINTER(ctypes.c_uint64)),
                 ("pool", ctypes.POINTER(ctypes.c_int32))]
+
+
+class KvDescription(ctypes.Structure):
+    """pr_kv: a KV cache in the caller's device memory."""
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("layers", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("num_slots", ctypes.c_int32), ("slot_pages", ctypes.c_int32),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_layer", ctypes.c_int64), ("k_page", ctypes.c_int64),
+                ("v_layer", ctypes.c_int64), ("v_page", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("skipped", ctypes.c_void_p)]
 
 
 _lib_handle = None
@@ -111,6 +125,19 @@ def lib() -> ctypes.CDLL:
     L.pr_forest_info_get.restype = ctypes.c_int32
     L.pr_forest_host_image.argtypes = [_vp, ctypes.POINTER(ImageView)]
     L.pr_forest_host_image.restype = ctypes.c_int32
+    i32, i64, kv = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(KvDescription)
+    for name, args in (("pr_kv_init", [kv, _vp]),
+                       ("pr_kv_workspace", [kv, i32, i64, i64, _i64p]),
+                       ("pr_kv_extend", [kv, _vp, _vp, i64, i64, _vp, _vp, i64, _vp]),
+                       ("pr_kv_write", [kv, i32, _vp, _vp, i64, _vp, i64, i64, i32, _vp]),
+                       ("pr_kv_attend", [kv, i32, _vp, i64, _vp, i64, i32, i32, ctypes.c_float, i32, _vp, _vp, _vp,
+                                         i64, _vp]),
+                       ("pr_kv_fork", [kv, _vp, _vp, _vp, i64, _vp]),
+                       ("pr_kv_trim", [kv, _vp, _vp, i64, i64, _vp]),
+                       ("pr_kv_compact", [kv, _vp, _vp, i64, _vp]),
+                       ("pr_kv_check", [kv, _vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = i32
     if L.pr_abi_version() != 7:
         raise RuntimeError("libprefix_router ABI version mismatch")
     _lib_handle = L
