@@ -91,60 +91,85 @@ __device__ __forceinline__ float rows_sum(float x) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Where a workgroup works: which entry, and which of its chunks.
+// Sum of v over the lanes up to this one.
+__device__ __forceinline__ int32_t lanes_upto(int32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // the lane 1, 2, 4, 8 before, in each 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the 16 lanes before, into the second and fourth
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the first half, into the second
+    return v;
+}
+
+// Where a workgroup works: an entry (-1: nowhere), and which of its chunks.
 struct KvUnit {
-    int32_t entry, chunk, chunks, first_unit, chunk_tokens;
+    int32_t entry, slot, length, chunk, chunks, first_unit, chunk_tokens;
 };
 
-__device__ __forceinline__ int32_t kv_entry_length(const KvView &c, const int32_t *slots, int64_t i) {
-    const int32_t s = slots[i];
-    return kv_slot_ok(c, s) ? kv_length(c, s) : 0;
+// A slot's tokens; none for a slot that is none.
+__device__ __forceinline__ int32_t kv_known_length(const KvView &c, int32_t slot) {
+    return kv_slot_ok(c, slot) ? kv_length(c, slot) : 0;
 }
 
 // Unit u of the batch's chunks in the order of its entries, found by every wave
-// for itself from the lengths (a batch of at most kKvScan entries: four a lane).
-// entry is -1 past the last unit.
+// for itself from the lengths (a batch of at most kKvScan entries: E * 64).  A
+// kernel before this one that wrote the same down took longer than the two loads
+// and a dozen lane operations that it saved (see kv_plan_kernel).
+template <int E>
 __device__ inline KvUnit kv_find_unit(const KvAttend &a, int32_t u) {
     const int lane = (int)(threadIdx.x & 63);
-    int32_t span[kKvScan / 64];
-    int64_t total = 0;
+    int32_t slot[E], length[E], span[E], mine[E], total = 0;
 #pragma unroll
-    for (int e = 0; e < kKvScan / 64; ++e) {
-        const int32_t i = e * 64 + lane;
-        span[e] = i < a.n ? kv_span(kv_entry_length(a.c, a.slots, i), a.window) : 0;
-        total += span[e];
+    for (int e = 0; e < E; ++e) slot[e] = e * 64 + lane < a.n ? a.slots[e * 64 + lane] : -1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        length[e] = kv_known_length(a.c, slot[e]);
+        span[e] = kv_span(length[e], a.window);
+        total += kv_blocks(span[e]);
     }
-    for (int s = 32; s; s >>= 1) total += __shfl_xor((long long)total, s);
-    KvUnit r{-1, 0, 0, 0, kv_chunk_tokens(total, a.chunks, a.least)};
+    int32_t most = kv_chunk_tokens(__builtin_amdgcn_readlane(lanes_upto(total), 63), a.split);
+    // Chunks that end short may be more than the GPU holds at once: longer ones then,
+    // if that puts all of them into one turn.
+    int tries = a.n < a.split.fill && most <= a.split.worth ? 3 : 0;
+    for (;;) {
+        int32_t units = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            mine[e] = e * 64 + lane < a.n ? kv_chunks(span[e], most) : 0;
+            units += mine[e];
+        }
+        if (tries-- <= 0) break;
+        units = __builtin_amdgcn_readlane(lanes_upto(units), 63);
+        if (units <= a.split.fill) break;
+        most = kv_longer_chunk(most, units, a.split.fill);
+    }
+    KvUnit r{-1, -1, 0, 0, 0, 0, 0};
     int32_t before = 0;
 #pragma unroll
-    for (int e = 0; e < kKvScan / 64; ++e) {
-        if (e * 64 >= a.n) break;
-        const int32_t mine = e * 64 + lane < a.n ? kv_chunks(span[e], r.chunk_tokens) : 0;
-        int32_t upto = mine;
-        for (int s = 1; s < 64; s <<= 1) {
-            const int32_t o = __shfl_up(upto, s);
-            if (lane >= s) upto += o;
-        }
-        upto += before;
+    for (int e = 0; e < E; ++e) {
+        const int32_t upto = before + lanes_upto(mine[e]);
         const uint64_t past = __ballot(upto > u);
         if (past && r.entry < 0) {
             const int src = __builtin_ctzll(past);
             r.entry = e * 64 + src;
-            r.chunks = __builtin_amdgcn_readlane(mine, src);
+            r.slot = __builtin_amdgcn_readlane(slot[e], src);
+            r.length = __builtin_amdgcn_readlane(length[e], src);
+            r.chunks = __builtin_amdgcn_readlane(mine[e], src);
             r.first_unit = __builtin_amdgcn_readlane(upto, src) - r.chunks;
             r.chunk = u - r.first_unit;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
     }
+    r.chunk_tokens = kv_even_chunk(kv_span(r.length, a.window), r.chunks);
     return r;
 }
 
-// The same from a plan (kv_plan_kernel) for larger batches: a.plan[0] is the chunk's
-// tokens, a.plan[1 + i] the units before entry i.
+// The same from a plan (kv_plan_kernel) for larger batches: a.plan[i] is the units
+// before entry i.
 __device__ inline KvUnit kv_planned_unit(const KvAttend &a, int32_t u) {
-    const int32_t *before = a.plan + 1;
-    KvUnit r{-1, 0, 0, 0, a.plan[0]};
+    const int32_t *before = a.plan;
+    KvUnit r{-1, -1, 0, 0, 0, 0, 0};
     if (u >= before[a.n]) return r;
     int32_t lo = 0, hi = (int32_t)a.n;  // before[lo] <= u < before[hi]
     while (hi - lo > 1) {
@@ -153,9 +178,22 @@ __device__ inline KvUnit kv_planned_unit(const KvAttend &a, int32_t u) {
         else hi = mid;
     }
     r.entry = lo;
+    r.slot = a.slots[lo];
+    r.length = kv_known_length(a.c, r.slot);
     r.first_unit = before[lo];
     r.chunks = before[lo + 1] - r.first_unit;
     r.chunk = u - r.first_unit;
+    r.chunk_tokens = kv_even_chunk(kv_span(r.length, a.window), r.chunks);
+    return r;
+}
+
+// Where no entry can have two chunks, unit u is entry u.
+__device__ inline KvUnit kv_whole_unit(const KvAttend &a, int32_t u) {
+    KvUnit r{-1, -1, 0, 0, 1, u, kKvMostTokens};
+    if (u >= a.n) return r;
+    r.entry = u;
+    r.slot = a.slots[u];
+    r.length = kv_known_length(a.c, r.slot);
     return r;
 }
 
@@ -179,11 +217,13 @@ __global__ void __launch_bounds__(1024) kv_plan_kernel(KvAttend a);
 // once for what that left over, so that the sum's terms are good to about 2^-17
 // (bf16) or 2^-22 (f16) and the output's error is its own rounding; the second
 // MFMA costs nothing next to the loads.
-template <typename IO, bool E4M3, int D, int R>
-__global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
+template <typename IO, bool E4M3, int D, int R, int W>
+__global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_kernel(KvAttend a) {
     using Raw = typename Eight<IO, E4M3>::Raw;
     constexpr int KB = D / 32;  // MFMAs of a score; pairs of 16 dimensions
     constexpr int ACC = D / 4;  // output numbers a lane holds for a row
+    constexpr int kStep = kKvTile * W;
+    constexpr float kSlack = 8.f;
     constexpr int SZ = E4M3 ? 1 : 2;
     const KvView &c = a.c;
     const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
@@ -192,18 +232,19 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
     // Blocks of the same keys differ by 8, so that they share an XCD's L2.
     const int32_t rg = (int32_t)((blockIdx.x >> 3) % (unsigned)a.row_groups);
     const int32_t uh = (int32_t)((blockIdx.x >> 3) / (unsigned)a.row_groups * 8 + (blockIdx.x & 7));
-    const int32_t unit = uh / c.kv_heads, head = uh % c.kv_heads;
-    // without a.where every entry is one unit
-    const KvUnit w = !a.where ? KvUnit{unit < a.n ? unit : -1, 0, 1, unit, kKvMostTokens}
-                     : a.plan ? kv_planned_unit(a, unit) : kv_find_unit(a, unit);
+    const int32_t unit = (int32_t)((uint32_t)uh / (uint32_t)c.kv_heads), head = uh - unit * c.kv_heads;
+    const KvUnit w = !a.where       ? kv_whole_unit(a, unit)
+                     : a.plan       ? kv_planned_unit(a, unit)
+                     : a.n <= 64    ? kv_find_unit<1>(a, unit)
+                     : a.n <= 128   ? kv_find_unit<2>(a, unit)
+                                    : kv_find_unit<kKvScan / 64>(a, unit);
     if (w.entry < 0) return;
     const int32_t entry = uniform(w.entry), chunks = uniform(w.chunks), chunk = uniform(w.chunk);
-    const int32_t slot = uniform(a.slots[entry]);
+    const int32_t slot = uniform(w.slot), length = uniform(w.length);
     const bool known = kv_slot_ok(c, slot);
-    const int32_t length = known ? uniform(kv_length(c, slot)) : 0;
     const int32_t begin = kv_first(length, a.window);
-    const int32_t from = (begin & ~(kKvTile - 1)) + chunk * w.chunk_tokens;
-    const int32_t to = (int32_t)min((int64_t)length, (int64_t)from + w.chunk_tokens);
+    const int32_t tokens = uniform(w.chunk_tokens), from = (begin & ~(kKvTile - 1)) + chunk * tokens;
+    const int32_t to = (int32_t)min((int64_t)length, (int64_t)from + tokens);
     if (chunk == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
         if (a.where) {
             a.where[2 * (int64_t)entry] = uniform(w.first_unit);
@@ -242,29 +283,48 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
         for (int j = 0; j < KB; ++j) o[r][j][0] = o[r][j][1] = f32x4{0, 0, 0, 0};
     }
 
-    const int32_t *pages = c.table + (int64_t)(known ? slot : 0) * c.slot_pages;
+    // Page ids are read by scalar loads: as vector loads they would be waited for
+    // behind every key and value on its way.
+    using Scalar = const __attribute__((address_space(4))) int32_t;
+    Scalar *pages = (Scalar *)(uintptr_t)(c.table + (int64_t)(known ? slot : 0) * c.slot_pages);
     const int32_t inside = kv_page_tokens(c) - 1;
     const char *kbase = (const char *)c.k + SZ * (a.layer * c.k_layer + kv_head_base(c, head));
     const char *vbase = (const char *)c.v + SZ * (a.layer * c.v_layer + kv_head_base(c, head));
 
-    for (int32_t t = from + kKvTile * wave; t < to; t += kKvStep) {
-        // the tile's two halves of 16 tokens, each in one page
-        int32_t pg[2];
-        bool good[2];
-        Raw kr[2][KB], vr[2][KB];
+    // A tile's two halves of 16 tokens lie in one page each.  The next tile's keys are
+    // asked for once this one's scores are taken, its values once this one's are used:
+    // the registers are free by then, and the rest of the tile's work hides the way.
+    Raw kr[2][KB], vr[2][KB];
+    auto page_of = [&](int32_t tok) { return tok < to ? pages[tok >> c.page_shift] : -1; };
+    const uint32_t kl = (uint32_t)SZ * kv_key_at(c, col, 8 * g), vl = (uint32_t)SZ * kv_value_at(c, 4 * g, 2 * col);
+    auto load_keys = [&](int32_t t, const int32_t *pg) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int32_t tok = t + 16 * h;
-            pg[h] = tok < to ? uniform(pages[tok >> c.page_shift]) : -1;
-            good[h] = kv_page_ok(c, pg[h]);
-            const int64_t p = good[h] ? pg[h] : 0;
-            const char *ks = kbase + SZ * (p * c.k_page + kv_key_at(c, (tok & inside) + col, 8 * g));
-            const char *vs = vbase + SZ * (p * c.v_page + kv_value_at(c, (tok & inside) + 4 * g, 2 * col));
+            const int64_t p = kv_page_ok(c, pg[h]) ? pg[h] : 0;
+            const char *ks = kbase + SZ * (p * c.k_page + kv_key_at(c, (t + 16 * h) & inside, 0));
 #pragma unroll
-            for (int j = 0; j < KB; ++j) kr[h][j] = *(const Raw *)(ks + SZ * ((int64_t)32 * j << c.page_shift));
-#pragma unroll
-            for (int j = 0; j < KB; ++j) vr[h][j] = *(const Raw *)(vs + SZ * 128 * j);
+            for (int j = 0; j < KB; ++j) kr[h][j] = *(const Raw *)(ks + (SZ * 32 * j << c.page_shift) + kl);
         }
+    };
+    auto load_values = [&](int32_t t, const int32_t *pg) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t p = kv_page_ok(c, pg[h]) ? pg[h] : 0;
+            const char *vs = vbase + SZ * (p * c.v_page + kv_value_at(c, (t + 16 * h) & inside, 0));
+#pragma unroll
+            for (int j = 0; j < KB; ++j) vr[h][j] = *(const Raw *)(vs + SZ * 128 * j + vl);
+        }
+    };
+    int32_t t = from + kKvTile * wave;
+    int32_t here[2] = {page_of(t), page_of(t + 16)};
+    int32_t next[2] = {page_of(t + kStep), page_of(t + kStep + 16)};
+    if (t < to) {
+        load_keys(t, here);
+        load_values(t, here);
+    }
+    for (; t < to; t += kStep) {
+        const bool good[2] = {kv_page_ok(c, here[0]), kv_page_ok(c, here[1])};
+        const bool more = t + kStep < to;
         const bool full = good[0] && good[1] && t >= begin && t + kKvTile <= to;
         u32x4 keep{~0u, ~0u, ~0u, ~0u};  // weights of tokens that count: two 16-bit ones a word
         if (!full) {
@@ -290,6 +350,7 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) s[r][h] = IO::mfma(kk, q[r][j], s[r][h]);
                 }
+            if (more) load_keys(t + kStep, next);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float x[8], top = -INFINITY;
@@ -299,28 +360,32 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
                     if (!full && !((keep[i / 2] >> (16 * (i & 1))) & 1)) x[i] = -INFINITY;
                     top = fmaxf(top, x[i]);
                 }
-                const float next = fmaxf(m[r], rows_max(top));
-                const float base = next == -INFINITY ? 0.f : next;  // nothing yet, or nothing but -infinity
-                const float shrink = exp2_fast(m[r] - base);
-                m[r] = next;
+                top = rows_max(top);
+                // m follows the maximum only once that is kSlack past it: until then weights
+                // up to 2^kSlack do no harm, and rescaling costs as much as a tile's scores
+                if (__ballot(!(top <= m[r] + kSlack))) {
+                    const float most = fmaxf(m[r], top), base = most == -INFINITY ? 0.f : most;
+                    const float shrink = exp2_fast(m[r] - base);
+                    m[r] = most;
+                    l[r] *= shrink;
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        o[r][j][0] *= shrink;
+                        o[r][j][1] *= shrink;
+                    }
+                }
+                const float base = m[r] == -INFINITY ? 0.f : m[r];  // nothing yet, or nothing but -infinity
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     x[i] = exp2_fast(x[i] - base);
                     sum += x[i];
                 }
-                l[r] = l[r] * shrink + sum;
+                l[r] += sum;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     hi[r][i] = IO::pack(x[2 * i], x[2 * i + 1]);
                     lo[r][i] = IO::pack(x[2 * i] - IO::low(hi[r][i]), x[2 * i + 1] - IO::high(hi[r][i]));
-                }
-                if (__ballot(!(shrink == 1.f))) {
-#pragma unroll
-                    for (int j = 0; j < KB; ++j) {
-                        o[r][j][0] *= shrink;
-                        o[r][j][1] *= shrink;
-                    }
                 }
             }
         }
@@ -338,15 +403,21 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
                 }
             }
         }
+        if (more) load_values(t + kStep, next);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            here[h] = next[h];
+            next[h] = page_of(t + 2 * kStep + 16 * h);
+        }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) l[r] = rows_sum(l[r]);
 
-    // join the waves: 2 and 3 into 0 and 1, 1 into 0
-    __shared__ f32x4 so[2][R * ACC / 4][64];
-    __shared__ float sm[2][R][64], sl[2][R][64];
+    // join the waves: the upper half into the lower, and again
+    __shared__ f32x4 so[W / 2][R * ACC / 4][64];
+    __shared__ float sm[W / 2][R][64], sl[W / 2][R][64];
 #pragma unroll
-    for (int half = 2; half; half >>= 1) {
+    for (int half = W / 2; half; half >>= 1) {
         if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -408,50 +479,78 @@ __global__ void __launch_bounds__(64 * kKvWaves) kv_attend_kernel(KvAttend a) {
     }
 }
 
-// Joins the chunks of one entry's row: workgroup = (entry, query head), its
-// threads a group of four dimensions each, the chunks dealt to as many teams.
-template <typename IO, int D>
+// Joins the chunks of entries that have more than one.  A row's numbers are dealt to
+// D / 4 threads; a workgroup takes ROWS query heads of an entry with as many teams as
+// are left over, each with a part of the chunks: one row where few are to be joined
+// (they have the most chunks), eight where many are (mostly to find that there is
+// nothing to join: 3,584 workgroups that only leave take 5 us to start).
+template <typename IO, int D, bool MANY>
 __global__ void __launch_bounds__(256) kv_join_kernel(KvAttend a) {
-    constexpr int COLS = D / 4, TEAMS = 256 / COLS;
-    const int64_t entry = blockIdx.x / (unsigned)a.q_heads, row = blockIdx.x % (unsigned)a.q_heads;
+    constexpr int COLS = D / 4, SETS = 256 / COLS, ROWS = MANY ? SETS : 1, TEAMS = SETS / ROWS;
+    const int32_t per_entry = (a.q_heads + ROWS - 1) / ROWS;
+    const int64_t entry = blockIdx.x / (unsigned)per_entry;
     const int32_t first = a.where[2 * entry], chunks = a.where[2 * entry + 1];
     if (chunks <= 1) return;
-    const int cgrp = (int)threadIdx.x % COLS, team = (int)threadIdx.x / COLS;
+    const int col = (int)threadIdx.x % COLS, set = (int)threadIdx.x / COLS, team = set / ROWS;
+    const int32_t row = (int32_t)(blockIdx.x % (unsigned)per_entry) * ROWS + set % ROWS;
+    const bool in = team < TEAMS && row < a.q_heads;
     __shared__ f32x4 so[TEAMS][COLS];
     __shared__ float sml[TEAMS][2];
     float m = -INFINITY, l = 0.f;
     f32x4 o{0, 0, 0, 0};
-    if (team < TEAMS) {
-        for (int32_t k = team; k < chunks; k += TEAMS) {
-            const int64_t at = (int64_t)(first + k) * a.q_heads + row;
-            const float2 ml = *(const float2 *)(a.part_ml + 2 * at);
-            const f32x4 po = *(const f32x4 *)(a.part_o + at * D + 4 * cgrp);
-            const float next = fmaxf(m, ml.x), base = next == -INFINITY ? 0.f : next;
-            const float x = exp2_fast(m - base), y = exp2_fast(ml.x - base);
-            m = next;
-            l = l * x + ml.y * y;
-            o = o * x + po * y;
-        }
-        so[team][cgrp] = o;
-        if (cgrp == 0) {
-            sml[team][0] = m;
-            sml[team][1] = l;
-        }
-    }
-    __syncthreads();
-    if (team) return;
+    if (in) {
+        constexpr int UP = 4;  // chunks whose numbers are on their way at once
+        for (int32_t k0 = team; k0 < chunks; k0 += UP * TEAMS) {
+            float2 ml[UP];
+            f32x4 po[UP];
+            float most = m;
 #pragma unroll
-    for (int k = 1; k < TEAMS; ++k) {
-        const float om = sml[k][0], next = fmaxf(m, om), base = next == -INFINITY ? 0.f : next;
-        const float x = exp2_fast(m - base), y = exp2_fast(om - base);
-        m = next;
-        l = l * x + sml[k][1] * y;
-        o = o * x + so[k][cgrp] * y;
+            for (int i = 0; i < UP; ++i) {
+                const int32_t k = k0 + i * TEAMS;
+                const int64_t at = (int64_t)(first + (k < chunks ? k : k0)) * a.q_heads + row;
+                ml[i] = *(const float2 *)(a.part_ml + 2 * at);
+                po[i] = *(const f32x4 *)(a.part_o + at * D + 4 * col);
+                if (k >= chunks) ml[i] = make_float2(-INFINITY, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < UP; ++i) most = fmaxf(most, ml[i].x);
+            const float base = most == -INFINITY ? 0.f : most, x = exp2_fast(m - base);
+            m = most;
+            l *= x;
+            o *= x;
+#pragma unroll
+            for (int i = 0; i < UP; ++i) {
+                if (k0 + i * TEAMS >= chunks) break;
+                const float y = exp2_fast(ml[i].x - base);
+                l += ml[i].y * y;
+                o += po[i] * y;
+            }
+        }
     }
+    if (TEAMS > 1) {
+        if (in) {
+            so[team][col] = o;
+            if (col == 0) {
+                sml[team][0] = m;
+                sml[team][1] = l;
+            }
+        }
+        __syncthreads();
+        if (team) return;
+#pragma unroll
+        for (int k = 1; k < TEAMS; ++k) {
+            const float om = sml[k][0], most = fmaxf(m, om), base = most == -INFINITY ? 0.f : most;
+            const float x = exp2_fast(m - base), y = exp2_fast(om - base);
+            m = most;
+            l = l * x + sml[k][1] * y;
+            o = o * x + so[k][col] * y;
+        }
+    }
+    if (!in) return;
     const int64_t to_row = entry * a.q_heads + row;
-    if (a.lse && cgrp == 0) a.lse[to_row] = (m + log2f(l)) * 0.6931471805599453f;
+    if (a.lse && col == 0) a.lse[to_row] = (m + log2f(l)) * 0.6931471805599453f;
     const float unit_v = a.c.v_scale / l;
-    *(u32x2 *)((uint32_t *)a.out + (to_row * D + 4 * cgrp) / 2) =
+    *(u32x2 *)((uint32_t *)a.out + (to_row * D + 4 * col) / 2) =
         u32x2{IO::pack(o[0] * unit_v, o[1] * unit_v), IO::pack(o[2] * unit_v, o[3] * unit_v)};
 }
 

@@ -11,17 +11,20 @@ hipError_t kv_launch_dim(const KvAttend &a, hipStream_t st) {
     // whole eights of (unit, key head) pairs, see the kernel's first lines
     const int64_t pairs = ((int64_t)a.units * a.c.kv_heads + 7) / 8 * 8;
     const dim3 grid((unsigned)(pairs * a.row_groups)), block(64 * kKvWaves);
-    if constexpr (D <= 192) {
-        if (kv_rows(a.group, D) == 2)
-            kv_attend_kernel<IO, E4M3, D, 2><<<grid, block, 0, st>>>(a);
-        else
-            kv_attend_kernel<IO, E4M3, D, 1><<<grid, block, 0, st>>>(a);
-    } else {
-        kv_attend_kernel<IO, E4M3, D, 1><<<grid, block, 0, st>>>(a);
-    }
+    const int rows = kv_rows(a.group, D);
+    if (a.wide)
+        kv_attend_kernel<IO, E4M3, D, 1, kv_wide(D)><<<grid, dim3(64 * kv_wide(D)), 0, st>>>(a);
+    else if (rows == 1)
+        kv_attend_kernel<IO, E4M3, D, 1, kKvWaves><<<grid, block, 0, st>>>(a);
+    else if constexpr (kv_rows(17, D) == 2)
+        kv_attend_kernel<IO, E4M3, D, 2, kKvWaves><<<grid, block, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.where) return e;
-    kv_join_kernel<IO, D><<<dim3((unsigned)(a.n * a.q_heads)), dim3(256), 0, st>>>(a);
+    constexpr int kSets = 256 / (D / 4);
+    if (a.n * a.q_heads > kKvJoinMany)
+        kv_join_kernel<IO, D, true><<<dim3((unsigned)(a.n * ((a.q_heads + kSets - 1) / kSets))), dim3(256), 0, st>>>(a);
+    else
+        kv_join_kernel<IO, D, false><<<dim3((unsigned)(a.n * a.q_heads)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -25,16 +25,33 @@ struct KvAttend {
     float *part_o, *part_ml;
     int64_t layer;
     int32_t q_heads, group, row_groups, window;
-    int32_t chunks, least;  // chunks a key head's tokens are cut into, and a chunk's least tokens
+    KvSplit split;          // of one key head's tokens
     int32_t units;          // chunks there may be at most
     float scale;            // with the keys' scale and log2 e
     bool q_aligned;
+    bool wide;  // one workgroup of many waves takes a sequence
 };
 
-// Rows of query heads a workgroup takes, in sixteens: two share the keys and values
-// that one would read twice; past 192 dimensions two rows' output does not fit the
-// registers next to a tile.
-constexpr int kv_rows(int group, int head_dim) { return group > 16 && head_dim <= 192 ? 2 : 1; }
+// Sixteens of query heads ("rows") a workgroup takes: two share the keys and values
+// that one would read twice, but past 128 dimensions two rows' output leaves room
+// for one wave a SIMD, which loses more (48 rows of 192 dimensions, e4m3: 60 us with
+// one, 86 with two).
+constexpr int kv_rows(int group, int head_dim) { return group > 16 && head_dim <= 128 ? 2 : 1; }
+
+// Waves a SIMD holds of the attention kernel, by its registers (and, of a workgroup
+// of many waves, at least its own).  One for 256 dimensions in 16 bits: two would
+// spill (64 sequences of 2,000 tokens, 4 key heads: 112 us with one, 124 with two).
+constexpr int kv_resident(bool e4m3, int head_dim, int rows, int waves) {
+    const int n = head_dim * rows;
+    const int chunked = e4m3 ? (n <= 64 ? 6 : (n <= 128 ? 4 : (n <= 192 ? 3 : 2)))
+                             : (n <= 64 ? 5 : (n <= 96 ? 4 : (n <= 128 ? 3 : (head_dim < 256 ? 2 : 1))));
+    return waves == kKvWaves ? chunked : waves / 4;
+}
+
+// Waves of a workgroup that takes a whole short sequence.
+constexpr int kv_wide(int head_dim) { return head_dim <= 96 ? 16 : 8; }
+
+constexpr int kKvJoinMany = 1024;  // rows from which a joining workgroup takes several
 
 hipError_t kv_launch_bf16(const KvAttend &a, bool e4m3, hipStream_t st);
 hipError_t kv_launch_f16(const KvAttend &a, bool e4m3, hipStream_t st);

@@ -53,7 +53,7 @@ PR_KV_FN int64_t kv_head_base(const KvView &c, int32_t head) {
 // ---- how attention splits a batch ---------------------------------------------
 constexpr int32_t kKvMostTokens = 1 << 30;  // of a sequence
 constexpr int kKvTile = 32;        // tokens a wave takes at a time
-constexpr int kKvWaves = 4;        // waves of a workgroup
+constexpr int kKvWaves = 4;        // waves of a workgroup that takes a chunk
 constexpr int kKvStep = kKvTile * kKvWaves;
 
 // First token attended, rounded down to a tile, and the tiles' tokens from there.
@@ -64,15 +64,45 @@ PR_KV_FN int32_t kv_span(int32_t length, int32_t window) {
     return length - (kv_first(length, window) & ~(kKvTile - 1));
 }
 
-// Tokens of a chunk: the batch's tokens over the chunks that fill the GPU, no
-// less than `least`, in whole steps of a workgroup.
-PR_KV_FN int32_t kv_chunk_tokens(int64_t tokens, int32_t chunks, int32_t least) {
-    int64_t c = (tokens + chunks - 1) / chunks;
-    c = (c + kKvStep - 1) / kKvStep * kKvStep;
-    return c < least ? least : (int32_t)c;
+// A span in blocks: 256 sequences' blocks can be added in 32 bits.
+constexpr int kKvBlock = 256;
+PR_KV_FN int32_t kv_blocks(int32_t span) { return (span + kKvBlock - 1) / kKvBlock; }
+
+// How a batch's tokens are cut: `fill` chunks occupy the GPU once; chunks longer
+// than `worth` are cut further, into `most` of them, for the sake of an even end;
+// no chunk is shorter than `least`.
+struct KvSplit {
+    int32_t fill, most, least, worth;
+};
+
+// Tokens a chunk has at most, in whole steps of a workgroup.
+PR_KV_FN int32_t kv_chunk_tokens(int32_t blocks, const KvSplit &s) {
+    const uint32_t steps = (uint32_t)blocks * (kKvBlock / kKvStep), worth = (uint32_t)(s.worth / kKvStep);
+    uint32_t c = (steps + (uint32_t)s.fill - 1) / (uint32_t)s.fill;
+    if (c > worth) {
+        const uint32_t cut = (steps + (uint32_t)s.most - 1) / (uint32_t)s.most;
+        c = cut > worth ? cut : worth;
+    }
+    if (c >= (uint32_t)kKvMostTokens / kKvStep) return kKvMostTokens;
+    return (int32_t)(c * kKvStep) < s.least ? s.least : (int32_t)(c * kKvStep);
 }
+// The chunk that makes about `fill` units of what `units` of length c were.
+PR_KV_FN int32_t kv_longer_chunk(int32_t c, int32_t units, int32_t fill) {
+    const uint64_t x = (uint64_t)((uint32_t)c / kKvStep) * (uint32_t)units / (uint32_t)fill + 1;
+    return x >= (uint64_t)kKvMostTokens / kKvStep ? kKvMostTokens : (int32_t)(x * kKvStep);
+}
+
 // Chunks of one sequence (one where it has no tokens: its output is written too).
-PR_KV_FN int32_t kv_chunks(int32_t span, int32_t chunk) { return span <= chunk ? 1 : (span + chunk - 1) / chunk; }
+PR_KV_FN int32_t kv_chunks(int32_t span, int32_t chunk) {
+    return span <= chunk ? 1 : (int32_t)(((uint32_t)span + (uint32_t)chunk - 1) / (uint32_t)chunk);
+}
+
+// A sequence's chunks made even.
+PR_KV_FN int32_t kv_even_chunk(int32_t span, int32_t chunks) {
+    if (chunks <= 1) return kKvMostTokens;
+    const uint32_t steps = ((uint32_t)span + kKvStep - 1) / kKvStep;
+    return (int32_t)((steps + (uint32_t)chunks - 1) / (uint32_t)chunks * kKvStep);
+}
 
 }  // namespace pr
 

@@ -518,27 +518,24 @@ __global__ void __launch_bounds__(256) kv_compact_move_kernel(KvCompact x, int32
 // ---- attention's split of large batches --------------------------------------------------
 __global__ void __launch_bounds__(kKvPlanThreads) kv_plan_kernel(KvAttend a) {
     const int tid = (int)threadIdx.x;
-    int64_t mine = 0, total = 0;
+    int64_t mine = 0, total = 0;  // blocks
     auto span = [&](int64_t i) {
         const int32_t s = a.slots[i];
         return kv_span(kv_slot_ok(a.c, s) ? kv_length(a.c, s) : 0, a.window);
     };
-    for (int64_t i = tid; i < a.n; i += kKvPlanThreads) mine += span(i);
+    for (int64_t i = tid; i < a.n; i += kKvPlanThreads) mine += kv_blocks(span(i));
     kv_block_before(mine, &total);
-    const int32_t chunk = kv_chunk_tokens(total, a.chunks, a.least);
+    const int32_t chunk = kv_chunk_tokens((int32_t)min(total, (int64_t)INT32_MAX / (kKvBlock / kKvStep)), a.split);
     int32_t before = 0;
     for (int64_t i0 = 0; i0 < a.n; i0 += kKvPlanThreads) {
         const int64_t i = i0 + tid;
         const int32_t cnt = i < a.n ? kv_chunks(span(i), chunk) : 0;
         int32_t all = 0;
         const int32_t at = before + kv_block_before(cnt, &all);
-        if (i < a.n) a.plan[1 + i] = at;
+        if (i < a.n) a.plan[i] = at;
         before += all;
     }
-    if (tid == 0) {
-        a.plan[0] = chunk;
-        a.plan[1 + a.n] = before;
-    }
+    if (tid == 0) a.plan[a.n] = before;
 }
 
 }  // namespace pr

@@ -143,29 +143,47 @@ int64_t compact_parts(const pr_kv *c, void *work, pr::KvCompact *x) {
     return p.bytes;
 }
 
-// How an attention is split: workgroups that fill the GPU, and the tokens that
-// are worth one.
-constexpr int kFill = 1024, kLeast = 256;
+#ifndef PR_KV_ROUNDS
+#define PR_KV_ROUNDS 4
+#endif
+#ifndef PR_KV_WORTH
+#define PR_KV_WORTH 1024
+#endif
+constexpr int kComputeUnits = 256, kRounds = PR_KV_ROUNDS, kWorth = PR_KV_WORTH;
 
 // The parts of an attention's split that go by the host's numbers (a.window and
 // the cache's sizes among them), and its workspace.
 int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window, void *work, pr::KvAttend *a) {
-    const int32_t group = q_heads / c->kv_heads, rows = 16 * pr::kv_rows(group, c->head_dim);
-    a->group = group;
-    a->q_heads = q_heads;
-    a->row_groups = (group + rows - 1) / rows;
-    a->chunks = std::max(1, kFill / (c->kv_heads * a->row_groups));
-    a->least = kLeast;
+    const bool e4m3 = c->dtype == PR_KV_E4M3;
+    const int32_t group = q_heads / c->kv_heads;
     int64_t span = (int64_t)c->slot_pages * c->page_tokens;
     if (window > 0) span = std::min<int64_t>(span, (int64_t)window + pr::kKvTile - 1);
-    const int64_t each = (span + kLeast - 1) / kLeast, units = std::min<int64_t>(n * each, a->chunks + n);
+    a->group = group;
+    a->q_heads = q_heads;
+    // Few sequences that cannot be long: a workgroup of many waves each, and nothing to
+    // join.  That takes less than a split where a wave has two tiles (one sequence of 611
+    // tokens, 14 heads of 64: 6.5 us, split 8.6; of 2,000: 10.4 and 8.8), or where the
+    // workgroups fill the GPU anyway (32 of 500 to 1,500 on 8 key heads of 128: 25.7, 30.0).
+    const int64_t pairs = n * c->kv_heads * ((group + 15) / 16);
+    const int32_t step = pr::kv_wide(c->head_dim) * pr::kKvTile;
+    a->wide = pairs <= kComputeUnits && span <= (pairs * 2 > kComputeUnits ? 8 : 2) * step;
+    const int32_t rows = a->wide ? 1 : pr::kv_rows(group, c->head_dim);
+    a->row_groups = (group + 16 * rows - 1) / (16 * rows);
+    const int32_t heads = c->kv_heads * a->row_groups;
+    const int32_t beside = kComputeUnits * pr::kv_resident(e4m3, c->head_dim, rows, pr::kKvWaves);
+    a->split.fill = std::max(1, beside / heads);
+    a->split.most = std::max(1, kRounds * beside / heads);
+    a->split.least = n * heads * 8 >= beside ? 512 : 256;
+    a->split.worth = kWorth;
+    const int64_t each = a->wide ? 1 : (span + a->split.least - 1) / a->split.least;
+    const int64_t units = std::min<int64_t>(n * each, a->split.most + n);
     a->units = (int32_t)std::min<int64_t>(units, INT32_MAX);
     a->where = a->plan = nullptr;
     a->part_ml = a->part_o = nullptr;
     if (each <= 1) return 0;
     Parts p(work);
     a->where = p.take<int32_t>(2 * n);
-    a->plan = n > pr::kKvScan ? p.take<int32_t>(n + 2) : nullptr;
+    a->plan = n > pr::kKvScan ? p.take<int32_t>(n + 1) : nullptr;
     a->part_ml = p.take<float>(units * q_heads * 2);
     a->part_o = p.take<float>(units * q_heads * c->head_dim);
     return p.bytes;

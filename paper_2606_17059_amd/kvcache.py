@@ -18,11 +18,6 @@ PR_KV_BF16, PR_KV_F16, PR_KV_E4M3 = 0, 1, 2
 PR_KV_WORK_EXTEND, PR_KV_WORK_ATTEND, PR_KV_WORK_COMPACT = 0, 1, 2
 
 
-def _io_code(dtype) -> int:
-    torch = _load_torch()
-    return {torch.bfloat16: PR_KV_BF16, torch.float16: PR_KV_F16}.get(dtype, -1)
-
-
 class KVCache:
     """A paged KV cache: keys and values, and who holds which page.
 
@@ -79,6 +74,11 @@ class KVCache:
             self.k_scale, self.v_scale, k.data_ptr() or None, v.data_ptr() or None, *strides, table.data_ptr() or None, lengths.data_ptr() or None, refs.data_ptr() or None,
             free.data_ptr() or None, skipped.data_ptr())
         self._ref = ctypes.byref(self._desc)
+        self._index, self._int32, self._int64 = k.device.index, torch.int32, torch.int64
+        # types that rows of new tokens and queries may have
+        self._io = {torch.bfloat16: PR_KV_BF16, torch.float16: PR_KV_F16} if k.dtype.itemsize == 1 else \
+            {k.dtype: codes[k.dtype]}
+        self._scale = 1.0 / math.sqrt(dim)
         self._bytes = {}
         self._lib = lib()
         self._work_bytes(PR_KV_WORK_COMPACT, 0, 0)  # refuses what is no cache
@@ -127,29 +127,34 @@ class KVCache:
             raise ValueError("stream must be of the cache's device")
         return _stream_ptr(stream, self.device)
 
-    def _ints(self, t, dtype, name, count=None):
+    def _ints(self, t, dtype, name, count=None) -> int:
+        """Checks a vector of integers; its length."""
         _dev(t, dtype, name)
-        if t.device != self.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{name} must be on the cache's device")
-        if t.dim() != 1 or (count is not None and t.shape[0] != count):
+        shape = t.shape
+        if len(shape) != 1 or (count is not None and shape[0] != count):
             raise ValueError(f"{name} must have one dimension" + (f" of {count}" if count is not None else ""))
-        return t
+        return shape[0]
 
     def _rows(self, t, name, count, heads):
-        """Rows of heads x head_dim numbers, contiguous but for a row stride."""
-        torch = _load_torch()
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        """Checks rows of heads x head_dim numbers, contiguous but for a row stride: (heads, row stride, type)."""
+        try:
+            index = t.get_device()
+            shape, stride, io = t.shape, t.stride(), self._io.get(t.dtype, -1)
+        except (AttributeError, RuntimeError):
+            index = -1
+        if index < 0:
             raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
-        if t.device != self.device:
+        if index != self._index:
             raise ValueError(f"{name} must be on the cache's device")
-        if t.dim() != 3 or t.shape[0] != count or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
+        if len(shape) != 3 or shape[0] != count or shape[2] != self.head_dim or (heads and shape[1] != heads):
             raise ValueError(f"{name} must be [{count}, {heads or 'heads'}, {self.head_dim}]")
-        if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim)):
+        if count and (stride[2] != 1 or (stride[1] != self.head_dim and shape[1] > 1)):
             raise ValueError(f"rows of {name} must be contiguous")
-        io = _io_code(t.dtype)
-        if io < 0 or (self._desc.dtype != PR_KV_E4M3 and t.dtype != self.dtype):
+        if io < 0:
             raise TypeError(f"{name} must be of the cache's type, or bfloat16 or float16 for a float8 cache")
-        return t, io
+        return shape[1], stride[0], io
 
     # ---- calls --------------------------------------------------------------------
     def init(self, stream=None) -> None:
@@ -159,18 +164,17 @@ class KVCache:
     def extend(self, slots, offsets, rows: int, place=None, stream=None):
         """Room for offsets[i + 1] - offsets[i] new tokens of each slots[i]: returns place, int32 [rows]
         (pr_kv_extend).  offsets is a device tensor, so `rows`, its last entry, is given beside it."""
-        torch = _load_torch()
-        self._ints(slots, torch.int32, "slots")
-        n = slots.shape[0]
-        self._ints(offsets, torch.int64, "offsets", n + 1)
+        n = self._ints(slots, self._int32, "slots")
+        self._ints(offsets, self._int64, "offsets", n + 1)
         if rows < 0:
             raise ValueError("rows must not be negative")
         st = self._st(stream)
         if place is None:
-            place = self._empty((rows,), torch.int32, stream)
-        self._ints(place, torch.int32, "place", rows)
+            place = self._empty((rows,), self._int32, stream)
+        else:
+            self._ints(place, self._int32, "place", rows)
         size = self._work_bytes(PR_KV_WORK_EXTEND, n, rows)
-        work = self._empty((size,), torch.uint8, stream)
+        work = self._empty((size,), _load_torch().uint8, stream)
         s = self._lib.pr_kv_extend(self._ref, slots.data_ptr() or None, offsets.data_ptr(), n, rows,
                                    place.data_ptr() or None, work.data_ptr() or None, size, st)
         if s != PR_OK:
@@ -179,15 +183,13 @@ class KVCache:
 
     def write(self, layer: int, place, k, v, stream=None) -> None:
         """Rows [rows, kv_heads, head_dim] of new tokens into their places in one layer (pr_kv_write)."""
-        torch = _load_torch()
-        self._ints(place, torch.int32, "place")
-        rows = place.shape[0]
-        k, io = self._rows(k, "k", rows, self.kv_heads)
-        v, vio = self._rows(v, "v", rows, self.kv_heads)
-        if io != vio:
+        rows = self._ints(place, self._int32, "place")
+        _, k_stride, io = self._rows(k, "k", rows, self.kv_heads)
+        _, v_stride, v_io = self._rows(v, "v", rows, self.kv_heads)
+        if io != v_io:
             raise TypeError("k and v must have one dtype")
-        s = self._lib.pr_kv_write(self._ref, layer, place.data_ptr() or None, k.data_ptr() or None, k.stride(0),
-                                  v.data_ptr() or None, v.stride(0), rows, io, self._st(stream))
+        s = self._lib.pr_kv_write(self._ref, layer, place.data_ptr() or None, k.data_ptr() or None, k_stride,
+                                  v.data_ptr() or None, v_stride, rows, io, self._st(stream))
         if s != PR_OK:
             _check(s)
 
@@ -197,10 +199,8 @@ class KVCache:
         the last `window` of them (pr_kv_attend).  scale: 1 / sqrt(head_dim) unless given.  lse: a float32
         tensor [n, heads] that gets the logarithm of the sum of exponentials."""
         torch = _load_torch()
-        self._ints(slots, torch.int32, "slots")
-        n = slots.shape[0]
-        q, io = self._rows(q, "q", n, 0)
-        heads = q.shape[1]
+        n = self._ints(slots, self._int32, "slots")
+        heads, stride, io = self._rows(q, "q", n, 0)
         st = self._st(stream)
         if out is None:
             out = self._empty((n, heads, self.head_dim), q.dtype, stream)
@@ -214,8 +214,8 @@ class KVCache:
                 raise ValueError("lse must be [n, heads] on the cache's device")
         size = self._work_bytes(PR_KV_WORK_ATTEND, n, heads)
         work = self._empty((size,), torch.uint8, stream) if size else None
-        s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, q.stride(0),
-                                   heads, io, 1.0 / math.sqrt(self.head_dim) if scale is None else scale, window,
+        s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, stride,
+                                   heads, io, self._scale if scale is None else scale, window,
                                    out.data_ptr() or None, lse.data_ptr() or None if lse is not None else None,
                                    work.data_ptr() if work is not None else None, size, st)
         if s != PR_OK:
@@ -224,11 +224,9 @@ class KVCache:
 
     def fork(self, src, dst, tokens, stream=None) -> None:
         """Empty slots dst[i] become the first tokens[i] tokens of src[i], sharing their pages (pr_kv_fork)."""
-        torch = _load_torch()
-        self._ints(src, torch.int32, "src")
-        n = src.shape[0]
-        self._ints(dst, torch.int32, "dst", n)
-        self._ints(tokens, torch.int32, "tokens", n)
+        n = self._ints(src, self._int32, "src")
+        self._ints(dst, self._int32, "dst", n)
+        self._ints(tokens, self._int32, "tokens", n)
         s = self._lib.pr_kv_fork(self._ref, src.data_ptr() or None, dst.data_ptr() or None,
                                  tokens.data_ptr() or None, n, self._st(stream))
         if s != PR_OK:
@@ -238,8 +236,7 @@ class KVCache:
         """Each slots[i] keeps its first keep[i] tokens, none without `keep` (pr_kv_trim).  keep may be a column of
         a route's match_len: a strided int32 vector."""
         torch = _load_torch()
-        self._ints(slots, torch.int32, "slots")
-        n = slots.shape[0]
+        n = self._ints(slots, self._int32, "slots")
         stride = 1
         if keep is not None:
             if not isinstance(keep, torch.Tensor) or not keep.is_cuda or keep.dtype != torch.int32:

@@ -40,9 +40,11 @@ static void one(std::mt19937 &rng) {
     const int n = kv_length(c, 0), window = pick(0, 2) ? 0 : pick(1, room + 9);
     CHECK(n >= 0 && n <= room);
     const int begin = kv_first(n, window), span = kv_span(n, window);
-    const int chunk = kv_chunk_tokens(pick(0, 1) ? span : 64 * (int64_t)span, pick(1, 64), pick(1, 2) * 256);
-    const int chunks = kv_chunks(span, chunk), head = pick(0, c.kv_heads - 1);
-    CHECK(chunk % kKvStep == 0 || chunk == 256);
+    KvSplit s{pick(1, 64), 0, pick(1, 2) * 256, pick(1, 8) * 256};
+    s.most = s.fill * pick(1, 4);
+    const int chunks = kv_chunks(span, kv_chunk_tokens((pick(0, 1) ? 1 : 64) * kv_blocks(span), s));
+    const int chunk = kv_even_chunk(span, chunks), head = pick(0, c.kv_heads - 1);
+    CHECK(chunk % kKvStep == 0);
     std::vector<int> keys((size_t)n * D), values((size_t)n * D), counted(n);
     const int part = D * T;  // elements of a head in a page
     for (int k = 0; k < chunks; ++k) {
@@ -98,18 +100,32 @@ static void one(std::mt19937 &rng) {
 // The split never makes more chunks than a launch has room for.
 static void split(std::mt19937 &rng) {
     auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); };
-    const int n = pick(1, 60), want = pick(1, 200), least = 256;
+    const int n = pick(1, 60);
+    KvSplit s{pick(1, 200), 0, 256, pick(1, 8) * 256};
+    s.most = s.fill * pick(1, 4);
     std::vector<int> spans(n);
-    int64_t total = 0, units = 0;
-    for (auto &s : spans) total += s = pick(0, 5) ? pick(0, 400) : pick(0, 200000);
-    const int chunk = kv_chunk_tokens(total, want, least);
-    for (int s : spans) {
-        CHECK(kv_chunks(s, chunk) == (s <= chunk ? 1 : (s + chunk - 1) / chunk));
-        CHECK((int64_t)kv_chunks(s, chunk) * chunk >= s);
-        CHECK(kv_chunks(s, chunk) <= std::max(1, (s + least - 1) / least));
-        units += kv_chunks(s, chunk);
+    int64_t units = 0;
+    int32_t total = 0;
+    for (auto &x : spans) total += kv_blocks(x = pick(0, 5) ? pick(0, 400) : pick(0, 200000));
+    int chunk = kv_chunk_tokens(total, s);
+    for (int tries = n < s.fill ? pick(0, 3) : 0; tries; --tries) {
+        int64_t now = 0;
+        for (int x : spans) now += kv_chunks(x, chunk);
+        const int longer = kv_longer_chunk(chunk, (int)now, s.fill);
+        CHECK(longer % kKvStep == 0 && longer >= kKvStep);
+        if (now > s.fill) {
+            CHECK(longer > chunk);
+            chunk = longer;
+        }
     }
-    CHECK(units <= (int64_t)want + n);
+    for (int x : spans) {
+        const int k = kv_chunks(x, chunk), even = kv_even_chunk(x, k);
+        CHECK(k == (x <= chunk ? 1 : (x + chunk - 1) / chunk));
+        CHECK((int64_t)k * even >= x && (k == 1 || even <= chunk));
+        CHECK(k <= std::max(1, (x + 255) / 256));
+        units += k;
+    }
+    CHECK(units <= (int64_t)s.most + n);
 }
 
 int main() {

@@ -104,7 +104,7 @@ def test_a_bad_argument_is_refused(name, index, value):
 def test_an_attention_that_splits_wants_its_workspace():
     from paper_2606_17059_amd import router as R
     L, need = R.lib(), ctypes.c_int64(0)
-    for slot_pages, splits in ((16, False), (17, True)):  # up to 256 tokens there is nothing to split
+    for slot_pages, splits in ((1, False), (16, False), (1 << 12, True)):  # short sequences are not split
         d = _desc(slot_pages=slot_pages)
         assert L.pr_kv_workspace(ctypes.byref(d), 1, 3, 4, ctypes.byref(need)) == R.PR_OK
         assert (need.value > 0) == splits
