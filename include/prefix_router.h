@@ -496,8 +496,10 @@ pr_status pr_kv_init(const pr_kv *c, void *hip_stream);
 #define PR_KV_WORK_EXTEND 0  /* n entries, m rows */
 #define PR_KV_WORK_ATTEND 1  /* n entries, m query heads */
 #define PR_KV_WORK_COMPACT 2 /* n and m are 0 */
+#define PR_KV_WORK_CHANGE 3  /* a fork or trim of n entries; m is 0 */
 
-/* Bytes (HOST, *bytes) of workspace that a call with these sizes needs. */
+/* Bytes (HOST, *bytes) of workspace that a call with these sizes needs (0: none,
+ * and its workspace may be NULL). */
 pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, int64_t *bytes);
 
 /*
@@ -558,7 +560,7 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
  * dst.  dst[i] -1 is padding.
  */
 pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
-                     void *hip_stream);
+                     void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /*
  * evictKVCache for a batch: sequence slots[i] keeps its first
@@ -571,7 +573,7 @@ pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, con
  * Skipped: slots out of range, negative keep.
  */
 pr_status pr_kv_trim(const pr_kv *c, const int32_t *slots, const int32_t *keep, int64_t keep_stride, int64_t n,
-                     void *hip_stream);
+                     void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /*
  * Move the held pages to the lowest ids: with L pages held, the j-th held page

@@ -91,17 +91,6 @@ __device__ __forceinline__ float rows_sum(float x) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Sum of v over the lanes up to this one.
-__device__ __forceinline__ int32_t lanes_upto(int32_t v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // the lane 1, 2, 4, 8 before, in each 16
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the 16 lanes before, into the second and fourth
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the first half, into the second
-    return v;
-}
-
 // Where a workgroup works: an entry (-1: nowhere), and which of its chunks.
 struct KvUnit {
     int32_t entry, slot, length, chunk, chunks, first_unit, chunk_tokens;

@@ -22,26 +22,40 @@ using kv_u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
 
 constexpr int kKvPlanThreads = 1024;
 
+// Sums that stop at 2^32 - 1: what is compared with a count of pages may be more
+// than any cache has.
+__device__ __forceinline__ uint32_t kv_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
 // Sum of v over the threads before this one, the workgroup's sum in *all.
-template <typename T>
-__device__ inline T kv_block_before(T v, T *all) {
-    __shared__ T part[kKvPlanThreads / 64];
+__device__ inline uint32_t kv_block_before(uint32_t v, uint32_t *all) {
+    __shared__ uint32_t part[kKvPlanThreads / 64];
     const int lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
-    T upto = v;
-    for (int s = 1; s < 64; s <<= 1) {
-        const T o = __shfl_up(upto, s);
-        if (lane >= s) upto += o;
-    }
+    const uint32_t upto = lanes_upto(v, kv_add);
     __syncthreads();
     if (lane == 63) part[wave] = upto;
     __syncthreads();
-    T before = 0, sum = 0;
+    uint32_t before = 0, sum = 0;
+#pragma unroll
     for (int i = 0; i < kKvPlanThreads / 64; ++i) {
-        if (i < wave) before += part[i];
-        sum += part[i];
+        if (i == wave) before = sum;
+        sum = kv_add(sum, part[i]);
     }
     *all = sum;
-    return before + upto - v;
+    return kv_add(before, upto - v);  // exact in the wave unless past everything
+}
+
+// Calls put(rank, page) for the set bits of the wave's 64 words: `bits` is a lane's word,
+// 64 * word its first page and `rank` the number of set bits in the words before.
+template <typename Put>
+__device__ inline void kv_each_bit(unsigned long long bits, int32_t word, uint32_t rank, Put put) {
+    const int lane = (int)(threadIdx.x & 63);
+    for (uint64_t some = __ballot(bits != 0); some; some &= some - 1) {
+        const int src = __builtin_ctzll(some);
+        const uint64_t w = readlane64(bits, src);
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)rank, src);
+        if (w >> lane & 1)
+            put(first + (uint32_t)__popcll(w & ((1ull << lane) - 1)), 64 * __builtin_amdgcn_readlane(word, src) + lane);
+    }
 }
 
 __global__ void __launch_bounds__(256) kv_init_kernel(KvView c) {
@@ -84,103 +98,127 @@ __device__ __forceinline__ unsigned long long kv_free_word(const KvView &c, int3
     return c.free_pages[w] & (in >= 64 ? ~0ull : (1ull << in) - 1);
 }
 
-// Tokens entry i appends, -1 if it is out of order or out of range.
-__device__ __forceinline__ int64_t kv_appended(const KvExtend &x, int64_t i) {
+// An entry of an extension: its slot (-1 if it is none), and the tokens it appends (-1
+// if its offsets are out of order or out of range).
+struct KvEntry {
+    int32_t slot;
+    int64_t add;
+};
+__device__ __forceinline__ KvEntry kv_entry(const KvExtend &x, int64_t i) {
+    if (i >= x.n) return KvEntry{-1, 0};
     const int64_t a = x.offsets[i], b = x.offsets[i + 1];
-    return a < 0 || b < a || b > x.rows ? -1 : b - a;
+    return KvEntry{x.slots[i], a < 0 || b < a || b > x.rows ? -1 : b - a};
 }
 
+// What an entry's sequence holds: its tokens, its last page if that is partly filled
+// (-1: no such page), and who holds that.
+struct KvTail {
+    int32_t start, last, holders;
+};
+__device__ __forceinline__ KvTail kv_tail(const KvView &c, const KvEntry &e) {
+    KvTail t{0, -1, 0};
+    if (!kv_slot_ok(c, e.slot) || e.add <= 0) return t;
+    t.start = kv_length(c, e.slot);
+    if (t.start & (kv_page_tokens(c) - 1)) t.last = c.table[(int64_t)e.slot * c.slot_pages + (t.start >> c.page_shift)];
+    if (kv_page_ok(c, t.last)) t.holders = c.refs[t.last];
+    return t;
+}
+
+// One workgroup.  The loads of the first 1,024 entries and words of free bits are
+// started before the first barrier: a batch of up to that many waits for memory
+// four times in a row (its slots, lengths, last pages, and their holders).
 __global__ void __launch_bounds__(kKvPlanThreads) kv_extend_plan_kernel(KvExtend x) {
     const KvView &c = x.c;
     const int tid = (int)threadIdx.x;
-    __shared__ int32_t copies, skipped, granted;
-    if (tid == 0) copies = skipped = granted = 0;
-    // a slot's first entry
-    for (int64_t i = tid; i < x.n; i += kKvPlanThreads)
-        if (kv_slot_ok(c, x.slots[i]) && kv_appended(x, i) > 0) x.owner[x.slots[i]] = INT32_MAX;
-    __syncthreads();
-    for (int64_t i = tid; i < x.n; i += kKvPlanThreads)
-        if (kv_slot_ok(c, x.slots[i]) && kv_appended(x, i) > 0) atomicMin(&x.owner[x.slots[i]], (int32_t)i);
-    // free pages
     const int32_t words = (c.num_pages + 63) / 64;
-    int32_t mine = 0, available = 0;
-    for (int32_t w = tid; w < words; w += kKvPlanThreads) mine += (int32_t)__popcll(kv_free_word(c, w));
+    __shared__ int32_t copies, skipped;
+    __shared__ uint32_t granted;
+    if (tid == 0) copies = skipped = granted = 0;
+    const KvEntry e0 = kv_entry(x, tid);
+    const unsigned long long w0 = tid < words ? kv_free_word(c, tid) : 0;
+    // a slot's first entry
+    auto claims = [&](const KvEntry &e) { return kv_slot_ok(c, e.slot) && e.add > 0; };
+    for (int64_t i = tid; i < x.n; i += kKvPlanThreads) {
+        const KvEntry e = i == tid ? e0 : kv_entry(x, i);
+        if (claims(e)) x.owner[e.slot] = INT32_MAX;
+    }
+    const KvTail t0 = kv_tail(c, e0);
+    __syncthreads();
+    for (int64_t i = tid; i < x.n; i += kKvPlanThreads) {
+        const KvEntry e = i == tid ? e0 : kv_entry(x, i);
+        if (claims(e)) atomicMin(&x.owner[e.slot], (int32_t)i);
+    }
+    // free pages
+    uint32_t mine = (uint32_t)__popcll(w0), available = 0;
+    for (int32_t w = tid + kKvPlanThreads; w < words; w += kKvPlanThreads) mine += (uint32_t)__popcll(kv_free_word(c, w));
     kv_block_before(mine, &available);
-    if (available > x.most) available = (int32_t)x.most;
+    if (available > x.most) available = (uint32_t)x.most;
     // pages each entry needs, in the order of the batch: the first that finds too few
     // left is refused, and with it every later one that needs a page
-    int64_t upto = 0;
+    uint32_t upto = 0;
     for (int64_t i0 = 0; i0 < x.n; i0 += kKvPlanThreads) {
         const int64_t i = i0 + tid;
-        KvGrant g{0, -1, -1};
-        int64_t need = 0, add = 0;
-        int32_t slot = -1;
-        if (i < x.n) {
-            slot = x.slots[i];
-            add = kv_appended(x, i);
-            if (kv_slot_ok(c, slot) && add >= 0 &&
-                (add == 0 || __hip_atomic_load(&x.owner[slot], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i)) {
-                g.start = kv_length(c, slot);
-                if (g.start + add <= (int64_t)c.slot_pages << c.page_shift) {
-                    g.slot = slot;
-                    const int32_t old = kv_pages(c, g.start);
-                    if (add > 0 && (g.start & (kv_page_tokens(c) - 1))) {
-                        const int32_t last = c.table[(int64_t)slot * c.slot_pages + old - 1];
-                        if (!kv_page_ok(c, last)) g.slot = -1;  // nothing to append to
-                        else if (c.refs[last] > 1) g.source = last;
-                    }
-                    if (g.slot >= 0) need = kv_pages(c, g.start + add) - old + (g.source >= 0);
-                }
-            }
+        const KvEntry e = i0 == 0 ? e0 : kv_entry(x, i);
+        const KvTail t = i0 == 0 ? t0 : kv_tail(c, e);
+        KvGrant g{t.start, -1, -1};
+        uint32_t need = 0;
+        if (e.add == 0 && kv_slot_ok(c, e.slot)) {
+            g.slot = e.slot;  // nothing to do, and nothing wrong
+        } else if (claims(e) &&
+                   __hip_atomic_load(&x.owner[e.slot], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
+                   t.start + e.add <= (int64_t)c.slot_pages << c.page_shift &&
+                   (kv_page_ok(c, t.last) || !(t.start & (kv_page_tokens(c) - 1)))) {
+            g.slot = e.slot;
+            if (t.holders > 1) g.source = t.last;
+            need = (uint32_t)(kv_pages(c, t.start + e.add) - kv_pages(c, t.start) + (g.source >= 0));
         }
-        int64_t asked = 0;
-        const int64_t before = upto + kv_block_before(need, &asked);
-        upto += asked;
+        uint32_t asked = 0;
+        const uint32_t before = kv_add(upto, kv_block_before(need, &asked)), after = kv_add(before, need);
+        upto = kv_add(upto, asked);
         if (need > 0) {
-            if (before + need > available) g.slot = g.source = -1;
-            else atomicMax(&granted, (int32_t)(before + need));
+            if (after > available) g.slot = g.source = -1;
+            else atomicMax(&granted, after);
         }
         if (i < x.n) {
-            if (g.slot < 0 && slot != -1) atomicAdd(&skipped, 1);
+            if (g.slot < 0 && e.slot != -1) atomicAdd(&skipped, 1);
             x.grant[i] = g;
             x.rank[i] = (int32_t)(before < INT32_MAX ? before : INT32_MAX);
             if (g.source >= 0) x.copies[atomicAdd(&copies, 1)] = (int32_t)i;
-            if (g.slot >= 0 && add > 0) c.lengths[g.slot] = g.start + (int32_t)add;
+            if (g.slot >= 0 && e.add > 0) c.lengths[g.slot] = g.start + (int32_t)e.add;
         }
     }
     __syncthreads();
     // the lowest free pages
-    int32_t seen = 0;
-    for (int32_t w0 = 0; w0 < words && seen < granted; w0 += kKvPlanThreads) {
-        const int32_t w = w0 + tid;
-        const unsigned long long bits = w < words ? kv_free_word(c, w) : 0;
-        int32_t all = 0;
-        int32_t r = seen + kv_block_before((int32_t)__popcll(bits), &all);
-        unsigned long long left = bits;
-        for (; left && r < granted; ++r) {
-            const int32_t p = 64 * w + __builtin_ctzll(left);
-            left &= left - 1;
-            x.fresh[r] = p;
-            c.refs[p] = 1;
+    const uint32_t wanted = granted;
+    uint32_t seen = 0;
+    for (int32_t f = 0; f < words && seen < wanted; f += kKvPlanThreads) {
+        const int32_t w = f + tid;
+        const unsigned long long bits = f == 0 ? w0 : (w < words ? kv_free_word(c, w) : 0);
+        uint32_t all = 0;
+        const uint32_t r = seen + kv_block_before((uint32_t)__popcll(bits), &all);
+        // the word's first wanted - r free pages are taken
+        unsigned long long taken = r < wanted ? bits : 0;
+        if (taken && r + (uint32_t)__popcll(bits) > wanted) {
+            taken = 0;
+            unsigned long long left = bits;
+            for (uint32_t k = r; k < wanted; ++k, left &= left - 1) taken |= left & (~left + 1);
         }
-        if (left != bits) c.free_pages[w] = left;
+        kv_each_bit(taken, w, r, [&](uint32_t rank, int32_t p) {
+            x.fresh[rank] = p;
+            c.refs[p] = 1;
+        });
+        if (taken) c.free_pages[w] = bits & ~taken;
         seen += all;
     }
-    __syncthreads();
-    // copied pages have one holder less; the last one's leaving frees them
-    for (int32_t k = tid; k < copies; k += kKvPlanThreads) {
-        const int32_t p = x.grant[x.copies[k]].source;
-        if (atomicSub(&c.refs[p], 1) == 1) atomicOr(&c.free_pages[p >> 6], 1ull << (p & 63));
-    }
     if (tid == 0) {
-        x.count[0] = granted;
+        x.count[0] = (int32_t)wanted;
         x.count[1] = copies;
         if (skipped) atomicAdd(c.skipped, (unsigned long long)skipped);
     }
 }
 
 // Copies the first `tokens` tokens of page src to page dst, one (layer, head) of
-// keys or values, by one wave.
+// keys or values, by one wave, four units a lane on their way at once.
 template <typename T>
 __device__ inline void kv_copy_tokens(const T *src, T *dst, bool keys, int32_t tokens, const KvView &c) {
     using V8 = __attribute__((ext_vector_type(8))) T;
@@ -188,78 +226,98 @@ __device__ inline void kv_copy_tokens(const T *src, T *dst, bool keys, int32_t t
     const int32_t lane = (int32_t)(threadIdx.x & 63);
     if (keys) {
         const int32_t units = c.head_dim / 8 * tokens;
-        for (int32_t u = lane; u < units; u += 64) {
-            const int32_t at = kv_key_at(c, u % tokens, u / tokens * 8);
-            *(V8 *)(dst + at) = *(const V8 *)(src + at);
+        for (int32_t u0 = lane; u0 < units; u0 += 256) {
+            V8 x[4];
+            int32_t at[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t u = (uint32_t)(u0 + 64 * i), block = u / (uint32_t)tokens;
+                at[i] = kv_key_at(c, (int32_t)(u - block * (uint32_t)tokens), (int32_t)block * 8);
+                if (u < (uint32_t)units) x[i] = *(const V8 *)(src + at[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (u0 + 64 * i < units) *(V8 *)(dst + at[i]) = x[i];
         }
     } else {
-        const int32_t units = (tokens + 3) / 4 * c.head_dim;
-        for (int32_t u = lane; u < units; u += 64) {
-            const int32_t left = tokens - u / c.head_dim * 4;
-            if (left >= 4) {
-                *(V4 *)(dst + 4 * u) = *(const V4 *)(src + 4 * u);
-            } else {
-                for (int32_t e = 0; e < left; ++e) dst[4 * u + e] = src[4 * u + e];
-            }
+        const int32_t whole = tokens / 4 * c.head_dim, units = (tokens + 3) / 4 * c.head_dim;
+        for (int32_t u0 = lane; u0 < whole; u0 += 256) {
+            V4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (u0 + 64 * i < whole) x[i] = *(const V4 *)(src + 4 * (u0 + 64 * i));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (u0 + 64 * i < whole) *(V4 *)(dst + 4 * (u0 + 64 * i)) = x[i];
         }
+        for (int32_t u = whole + lane; u < units; u += 64)
+            for (int32_t e = 0; e < (tokens & 3); ++e) dst[4 * u + e] = src[4 * u + e];
     }
 }
 
-// The pages into the tables, each row's place, and the copies.
+// The last of the n numbers in a, which do not decrease, that is at most v (0 if none is).
+template <typename N>
+__device__ __forceinline__ int64_t kv_last_at_most(const N *a, int64_t n, int64_t v) {
+    int64_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (a[mid] <= v) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The first `row_blocks` workgroups: each row's place, the new pages into the tables,
+// and the copied pages' counts.  The others: the copies, a wave for each (layer, head, keys or values).
 template <typename T>
-__global__ void __launch_bounds__(256) kv_extend_place_kernel(KvExtend x) {
+__global__ void __launch_bounds__(256) kv_extend_place_kernel(KvExtend x, uint32_t row_blocks) {
     const KvView &c = x.c;
-    const int32_t pages = x.count[0], copies = x.count[1];
-    const int64_t step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    for (int64_t r = first; r < pages; r += step) {
-        int64_t lo = 0, hi = x.n;  // the last entry with rank[lo] <= r
-        while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (x.rank[mid] <= r) lo = mid;
-            else hi = mid;
-        }
-        const KvGrant g = x.grant[lo];
-        const int32_t at = kv_pages(c, g.start) - (g.source >= 0) + (int32_t)(r - x.rank[lo]);
-        if (g.slot >= 0 && (uint32_t)at < (uint32_t)c.slot_pages) c.table[(int64_t)g.slot * c.slot_pages + at] = x.fresh[r];
-    }
-    for (int64_t r = first; r < x.rows; r += step) {
-        if (x.n == 0) {
-            x.place[r] = -1;
-            continue;
-        }
-        int64_t lo = 0, hi = x.n;
-        if (x.rows == x.n && x.offsets[r] == r && x.offsets[r + 1] == r + 1) {
-            lo = r;  // a token each
-        } else {
-            while (hi - lo > 1) {  // the last entry that begins at or before r
-                const int64_t mid = (lo + hi) >> 1;
-                if (x.offsets[mid] <= r) lo = mid;
-                else hi = mid;
+    if (blockIdx.x < row_blocks) {
+        const int64_t step = (int64_t)row_blocks * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        for (int64_t r = first; r < x.rows; r += step) {
+            int32_t to = -1;
+            if (x.n > 0) {
+                // a token each, or the last entry that begins at or before r
+                const bool each = x.rows == x.n && x.offsets[r] == r && x.offsets[r + 1] == r + 1;
+                const int64_t i = each ? r : kv_last_at_most(x.offsets, x.n, r);
+                const KvGrant g = x.grant[i];
+                const int64_t a = x.offsets[i];
+                if (g.slot >= 0 && r >= a && r < x.offsets[i + 1]) {
+                    const int64_t pos = g.start + (r - a);
+                    const int32_t col = (int32_t)(pos >> c.page_shift), old = kv_pages(c, g.start) - (g.source >= 0);
+                    const int32_t page = col >= old ? x.fresh[x.rank[i] + col - old]
+                                                    : c.table[(int64_t)g.slot * c.slot_pages + col];
+                    if (kv_page_ok(c, page)) to = (page << c.page_shift) + (int32_t)(pos & (kv_page_tokens(c) - 1));
+                }
             }
+            x.place[r] = to;
         }
-        int32_t to = -1;
-        const KvGrant g = x.grant[lo];
-        const int64_t a = x.offsets[lo];
-        if (g.slot >= 0 && r >= a && r < x.offsets[lo + 1]) {
-            const int64_t pos = g.start + (r - a);
-            const int32_t col = (int32_t)(pos >> c.page_shift), old = kv_pages(c, g.start) - (g.source >= 0);
-            const int32_t page = col >= old ? x.fresh[x.rank[lo] + col - old] : c.table[(int64_t)g.slot * c.slot_pages + col];
-            if (kv_page_ok(c, page)) to = (page << c.page_shift) + (int32_t)(pos & (kv_page_tokens(c) - 1));
+        const int32_t pages = x.count[0];
+        for (int64_t r = first; r < pages; r += step) {
+            const int64_t i = kv_last_at_most(x.rank, x.n, r);
+            const KvGrant g = x.grant[i];
+            const int32_t at = kv_pages(c, g.start) - (g.source >= 0) + (int32_t)(r - x.rank[i]);
+            if (g.slot >= 0 && (uint32_t)at < (uint32_t)c.slot_pages)
+                c.table[(int64_t)g.slot * c.slot_pages + at] = x.fresh[r];
         }
-        x.place[r] = to;
+        // copied pages have one holder less; the last one's leaving frees them
+        for (int64_t k = first; k < x.count[1]; k += step) {
+            const int32_t p = x.grant[x.copies[k]].source;
+            if (atomicSub(&c.refs[p], 1) == 1) atomicOr(&c.free_pages[p >> 6], 1ull << (p & 63));
+        }
+        return;
     }
-    const int64_t items = (int64_t)copies * c.layers * c.kv_heads * 2;
-    for (int64_t it = first >> 6; it < items; it += step >> 6) {
-        const bool keys = it & 1;
-        int64_t y = it >> 1;
-        const int32_t head = (int32_t)(y % c.kv_heads);
-        y /= c.kv_heads;
-        const int32_t layer = (int32_t)(y % c.layers), i = x.copies[y / c.layers];
-        const KvGrant g = x.grant[i];
-        const int64_t at = layer * (keys ? c.k_layer : c.v_layer) + kv_head_base(c, head);
+    const uint32_t waves = (gridDim.x - row_blocks) * 4, each = (uint32_t)c.layers * (uint32_t)c.kv_heads * 2;
+    const uint64_t items = (uint64_t)(uint32_t)x.count[1] * each;
+    for (uint64_t it = (blockIdx.x - row_blocks) * 4 + (threadIdx.x >> 6); it < items; it += waves) {
+        const KvGrant g = x.grant[x.copies[it / each]];
+        const uint32_t y = (uint32_t)(it % each), layer = (y >> 1) / (uint32_t)c.kv_heads;
+        const bool keys = y & 1;
+        const int64_t at = layer * (keys ? c.k_layer : c.v_layer) +
+                           kv_head_base(c, (int32_t)((y >> 1) - layer * (uint32_t)c.kv_heads));
         T *pool = (T *)(keys ? c.k : c.v) + at;
         const int64_t page = keys ? c.k_page : c.v_page;
-        kv_copy_tokens<T>(pool + g.source * page, pool + x.fresh[x.rank[i]] * page, keys,
+        kv_copy_tokens<T>(pool + g.source * page, pool + x.fresh[x.rank[x.copies[it / each]]] * page, keys,
                           g.start & (kv_page_tokens(c) - 1), c);
     }
 }
@@ -320,114 +378,202 @@ __device__ __forceinline__ int32_t kv_place(const KvRows &x, int64_t r) {
     return p >= 0 && (p >> x.c.page_shift) < x.c.num_pages ? p : -1;
 }
 
-// A thread takes eight dimensions of a row: its key is 8 contiguous numbers; its
-// value's numbers lie 4 tokens apart, so the thread of a block's first token
-// writes all four of them where the batch has them in a row (prompts), and single
-// numbers otherwise (a decode step).  Four rows' threads lie side by side, so that
-// the keys of four tokens are written together.
+// A thread takes eight dimensions of a row's key: 8 contiguous numbers.  Of the value
+// it takes the same eight dimensions' single numbers, 4 tokens apart (a decode step);
+// where the batch has a block's four tokens in a row (prompts), it takes two of the
+// eight dimensions for all four, 8 contiguous numbers again.  Eight rows' threads lie
+// side by side, so that rows are read and keys are written 128 bytes at a time.
 template <typename P>
 __device__ inline void kv_write_eight(const KvRows &x, int64_t r, int32_t dim) {
     using T = typename P::T;
     using V8 = __attribute__((ext_vector_type(8))) T;
+    union Eight {
+        T e[8];
+        V8 v;
+    } one;
     const KvView &c = x.c;
     const int32_t p = kv_place(x, r);
     if (p < 0) return;
-    const int32_t head = dim / c.head_dim, d = dim % c.head_dim, t = p & (kv_page_tokens(c) - 1);
-    const int64_t page = p >> c.page_shift;
+    const int32_t head = (int32_t)((uint32_t)dim / (uint32_t)c.head_dim), d = dim - head * c.head_dim;
+    const int32_t t = p & (kv_page_tokens(c) - 1);
+    const int64_t page = p >> c.page_shift, lead = r - (p & 3);
+    const uint16_t *vrow = (const uint16_t *)x.v + dim;
     uint16_t in[8];
-    union {
-        T e[8];
-        V8 v;
-    } k;
-    kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, in);
-    P::put(in, c.k_scale, k.e);
-    *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = k.v;
-
-    const int64_t lead = r - (p & 3);
-    const int32_t q = p & ~3;
-    T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
     bool whole = true;
-    for (int e = 0; e < 4; ++e) whole &= kv_place(x, lead + e) == q + e;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) whole &= kv_place(x, lead + e) == (p & ~3) + e;
+
+    kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, in);
+    P::put(in, c.k_scale, one.e);
+    *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = one.v;
+
+    T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
     if (whole) {
-        if (p != q) return;
-        union {
-            T e[32];
-            V8 v[4];
-        } b;
+        const int32_t two = 2 * (p & 3);
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-            T one[8];
-            kv_load8((const uint16_t *)x.v + (r + e) * x.v_stride + dim, x.aligned, in);
-            P::put(in, c.v_scale, one);
-            for (int i = 0; i < 8; ++i) b.e[4 * i + e] = one[i];
+            const uint16_t *src = vrow + (lead + e) * x.v_stride + two;
+            const uint32_t w = x.aligned ? *(const uint32_t *)src : src[0] | (uint32_t)src[1] << 16;
+            in[e] = (uint16_t)w;
+            in[4 + e] = (uint16_t)(w >> 16);
         }
-        for (int i = 0; i < 4; ++i) *(V8 *)(dst + 8 * i) = b.v[i];
+        P::put(in, c.v_scale, one.e);
+        *(V8 *)(dst + 4 * two) = one.v;
     } else {
-        T one[8];
-        kv_load8((const uint16_t *)x.v + r * x.v_stride + dim, x.aligned, in);
-        P::put(in, c.v_scale, one);
-        for (int i = 0; i < 8; ++i) dst[4 * i + (p & 3)] = one[i];
+        kv_load8(vrow + r * x.v_stride, x.aligned, in);
+        P::put(in, c.v_scale, one.e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dst[4 * i + (p & 3)] = one.e[i];
     }
 }
 
 template <typename P>
 __global__ void __launch_bounds__(256) kv_write_kernel(KvRows x) {
-    const int32_t eights = x.c.kv_heads * x.c.head_dim / 8;
-    const int64_t items = (x.rows + 3) / 4 * 4 * eights;
-    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < items; id += (int64_t)gridDim.x * 256)
-        kv_write_eight<P>(x, id / (4 * eights) * 4 + (id & 3), (int32_t)(id % (4 * eights) >> 2) * 8);
+    const uint32_t eights = (uint32_t)(x.c.kv_heads * x.c.head_dim / 8);
+    const uint64_t items = (uint64_t)(x.rows + 7) / 8 * 8 * eights;
+    // Workgroup b runs on XCD b % 8: neighbouring rows, whose tokens share cache lines,
+    // go to the same one.  The grid is in eights.
+    const uint64_t each = gridDim.x / 8, b = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    for (uint64_t id = b * 256 + threadIdx.x; id < items; id += 8 * each * 256) {
+        const uint64_t set = items < (1ull << 32) ? (uint32_t)id / (8 * eights) : id / (8 * eights);
+        const uint32_t in = (uint32_t)(id - set * (8 * eights));
+        kv_write_eight<P>(x, (int64_t)(set * 8 + (in & 7)), (int32_t)(in >> 3) * 8);
+    }
 }
 
-// ---- forks and trims: a workgroup an entry -----------------------------------------
-__global__ void __launch_bounds__(256) kv_fork_kernel(KvView c, const int32_t *src, const int32_t *dst,
-                                                      const int32_t *tokens, int64_t n) {
+// ---- forks and trims ---------------------------------------------------------------
+// A workgroup an entry decides what becomes of it.  In small batches it also changes
+// the table and the counts, four pages a thread on their way at once.  In large ones
+// (see kKvShared) it leaves its pages to a second launch, in which a workgroup takes
+// 64 columns of all the entries' tables: forks of one sequence hold the same page in
+// the same column, so their changes of its count are joined first.  (256 forks of 3
+// sequences of 1,300 to 3,100 scattered pages change half a million counts, 20 a
+// nanosecond at best: 24 us; joined, 9,000 are left.)
+constexpr int kKvPageThreads = 1024, kKvPageTurn = 4;
+constexpr int64_t kKvShared = 1 << 17;  // pages of a batch's tables from which there is a second launch
+constexpr int kKvSharedEntries = 512;   // entries of one of its workgroups
+
+struct KvChange {
+    KvView c;
+    const int32_t *src, *dst, *count;  // fork: sources, forks, tokens; trim: -, slots, keep
+    int64_t stride, n;                 // of count
+    int2 *columns;                     // per entry: first and last column that changes (nullptr: small batch)
+};
+
+// What becomes of the pages of one entry's table row in columns [lo, hi).
+template <bool FORK>
+__device__ inline void kv_change_row(const KvChange &x, int64_t i, int32_t lo, int32_t hi) {
+    const KvView &c = x.c;
+    if (x.columns) {
+        if (threadIdx.x == 0) x.columns[i] = make_int2(lo, hi);
+        return;
+    }
+    int32_t *row = c.table + (int64_t)x.dst[i] * c.slot_pages;
+    const int32_t *from = FORK ? c.table + (int64_t)x.src[i] * c.slot_pages : row;
+    for (int32_t k0 = lo + (int32_t)threadIdx.x; k0 < hi; k0 += kKvPageThreads * kKvPageTurn) {
+        int32_t p[kKvPageTurn], held[kKvPageTurn];
+#pragma unroll
+        for (int e = 0; e < kKvPageTurn; ++e) p[e] = k0 + e * kKvPageThreads < hi ? from[k0 + e * kKvPageThreads] : -1;
+#pragma unroll
+        for (int e = 0; e < kKvPageTurn; ++e) {
+            if (k0 + e * kKvPageThreads < hi) row[k0 + e * kKvPageThreads] = FORK ? p[e] : -1;
+            held[e] = 0;
+            if (kv_page_ok(c, p[e])) {
+                if (FORK) atomicAdd(&c.refs[p[e]], 1);
+                else held[e] = atomicSub(&c.refs[p[e]], 1);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kKvPageTurn; ++e)
+            if (!FORK && held[e] == 1) atomicOr(&c.free_pages[p[e] >> 6], 1ull << (p[e] & 63));
+    }
+}
+
+__global__ void __launch_bounds__(kKvPageThreads) kv_fork_kernel(KvChange x) {
+    const KvView &c = x.c;
     const int64_t i = blockIdx.x;
-    const int32_t from = src[i], to = dst[i], keep = tokens[i];
-    if (to == -1) return;
+    const int32_t from = x.src[i], to = x.dst[i], keep = x.count[i];
     __shared__ int32_t clash;
     if (threadIdx.x == 0) clash = 0;
     __syncthreads();
-    for (int64_t k = threadIdx.x; k < n; k += 256)
-        if (dst[k] == from || (k < i && dst[k] == to)) clash = 1;
+    if (to != -1)
+        for (int64_t k = threadIdx.x; k < x.n; k += kKvPageThreads)
+            if (x.dst[k] == from || (k < i && x.dst[k] == to)) clash = 1;
     __syncthreads();
     // lengths[to] is read before this workgroup, the only one that may, writes it
-    const bool bad = clash || !kv_slot_ok(c, from) || !kv_slot_ok(c, to) || keep < 0 || keep > kv_length(c, from) ||
-                     c.lengths[to] != 0;
+    const bool ok = to != -1 && !clash && kv_slot_ok(c, from) && kv_slot_ok(c, to) && keep >= 0 &&
+                    keep <= kv_length(c, from) && c.lengths[to] == 0;
     __syncthreads();
-    if (bad) {
-        if (threadIdx.x == 0) atomicAdd(c.skipped, 1ull);
-        return;
+    if (threadIdx.x == 0) {
+        if (ok) c.lengths[to] = keep;
+        else if (to != -1) atomicAdd(c.skipped, 1ull);
     }
-    const int32_t pages = kv_pages(c, keep);
-    for (int32_t k = (int32_t)threadIdx.x; k < pages; k += 256) {
-        const int32_t p = c.table[(int64_t)from * c.slot_pages + k];
-        c.table[(int64_t)to * c.slot_pages + k] = p;
-        if (kv_page_ok(c, p)) atomicAdd(&c.refs[p], 1);
-    }
-    if (threadIdx.x == 0) c.lengths[to] = keep;
+    kv_change_row<true>(x, i, 0, ok ? kv_pages(c, keep) : 0);
 }
 
-__global__ void __launch_bounds__(256) kv_trim_kernel(KvView c, const int32_t *slots, const int32_t *keep,
-                                                      int64_t keep_stride) {
+__global__ void __launch_bounds__(kKvPageThreads) kv_trim_kernel(KvChange x) {
+    const KvView &c = x.c;
     const int64_t i = blockIdx.x;
-    const int32_t slot = slots[i], to = keep ? keep[i * keep_stride] : 0;
-    if (slot == -1) return;
-    if (!kv_slot_ok(c, slot) || to < 0) {
-        if (threadIdx.x == 0) atomicAdd(c.skipped, 1ull);
-        return;
-    }
+    const int32_t slot = x.dst[i], to = x.count ? x.count[i * x.stride] : 0;
+    const bool ok = kv_slot_ok(c, slot) && to >= 0;
     // of the entries that name a slot each frees what its own minimum cuts off
     __shared__ int32_t had;
-    if (threadIdx.x == 0) had = atomicMin(&c.lengths[slot], to);
-    __syncthreads();
-    const int32_t room = c.slot_pages << c.page_shift, was = min(had, room);
-    if (was <= to) return;
-    const int32_t last = kv_pages(c, was);
-    for (int32_t k = kv_pages(c, to) + (int32_t)threadIdx.x; k < last; k += 256) {
-        int32_t *at = &c.table[(int64_t)slot * c.slot_pages + k];
-        const int32_t p = *at;
-        *at = -1;
-        if (kv_page_ok(c, p) && atomicSub(&c.refs[p], 1) == 1) atomicOr(&c.free_pages[p >> 6], 1ull << (p & 63));
+    if (threadIdx.x == 0) {
+        had = ok ? atomicMin(&c.lengths[slot], to) : 0;
+        if (!ok && slot != -1) atomicAdd(c.skipped, 1ull);
     }
+    __syncthreads();
+    const int32_t was = min(had, c.slot_pages << c.page_shift);
+    if (ok && was > to) kv_change_row<false>(x, i, kv_pages(c, to), kv_pages(c, was));
+    else kv_change_row<false>(x, i, 0, 0);
+}
+
+// 64 columns of up to kKvSharedEntries entries' table rows: a lane a column, a wave
+// every sixteenth entry.  A column has places for the counts of 16 pages; what finds
+// none is changed by itself.
+template <bool FORK>
+__global__ void __launch_bounds__(kKvPageThreads) kv_change_columns_kernel(KvChange x) {
+    constexpr int PLACES = 16, WAVES = kKvPageThreads / 64;
+    const KvView &c = x.c;
+    __shared__ int32_t page[PLACES][64], count[PLACES][64];
+    const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
+    page[wave][lane] = -1;
+    count[wave][lane] = 0;
+    __syncthreads();
+    const int32_t col = (int32_t)blockIdx.x * 64 + lane;
+    const int64_t first = (int64_t)blockIdx.y * kKvSharedEntries, last = min(x.n, first + kKvSharedEntries);
+    auto change = [&](int32_t p, int32_t by) {
+        if (FORK) atomicAdd(&c.refs[p], by);
+        else if (atomicSub(&c.refs[p], by) == by) atomicOr(&c.free_pages[p >> 6], 1ull << (p & 63));
+    };
+    for (int64_t i0 = first + wave; i0 < last; i0 += WAVES * kKvPageTurn) {
+        int32_t p[kKvPageTurn];
+        int32_t *at[kKvPageTurn];
+#pragma unroll
+        for (int e = 0; e < kKvPageTurn; ++e) {
+            const int64_t i = i0 + e * WAVES;
+            const int2 r = i < last ? x.columns[i] : make_int2(0, 0);
+            p[e] = -1;
+            at[e] = nullptr;
+            if (col >= r.x && col < r.y) {
+                at[e] = c.table + (int64_t)x.dst[i] * c.slot_pages + col;
+                p[e] = FORK ? c.table[(int64_t)x.src[i] * c.slot_pages + col] : *at[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kKvPageTurn; ++e) {
+            if (!at[e]) continue;
+            *at[e] = FORK ? p[e] : -1;
+            if (!kv_page_ok(c, p[e])) continue;
+            int32_t *key = &page[p[e] & (PLACES - 1)][lane];
+            const int32_t was = atomicCAS(key, -1, p[e]);
+            if (was == -1 || was == p[e]) atomicAdd(&count[p[e] & (PLACES - 1)][lane], 1);
+            else change(p[e], 1);
+        }
+    }
+    __syncthreads();
+    static_assert(PLACES == WAVES, "a thread a place");
+    if (count[wave][lane]) change(page[wave][lane], count[wave][lane]);
 }
 
 // ---- compaction -----------------------------------------------------------------------
@@ -443,11 +589,11 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_compact_plan_kernel(KvCompa
     const KvView &c = x.c;
     const int tid = (int)threadIdx.x;
     const int32_t words = (c.num_pages + 63) / 64;
-    int32_t mine = 0, unheld = 0;
-    for (int32_t w = tid; w < words; w += kKvPlanThreads) mine += (int32_t)__popcll(kv_free_word(c, w));
+    uint32_t mine = 0, unheld = 0;
+    for (int32_t w = tid; w < words; w += kKvPlanThreads) mine += (uint32_t)__popcll(kv_free_word(c, w));
     kv_block_before(mine, &unheld);
-    const int32_t held = c.num_pages - unheld;
-    int32_t holes = 0, movers = 0;
+    const int32_t held = c.num_pages - (int32_t)unheld;
+    uint32_t holes = 0, movers = 0;
     for (int32_t w0 = 0; w0 < words; w0 += kKvPlanThreads) {
         const int32_t w = w0 + tid, page = 64 * w;
         unsigned long long hole = 0, move = 0;
@@ -459,16 +605,16 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_compact_plan_kernel(KvCompa
             hole = bits & below;
             move = ~bits & valid & ~below;
         }
-        int32_t all = 0;
-        int32_t r = holes + kv_block_before((int32_t)__popcll(hole), &all);
+        uint32_t all = 0;
+        uint32_t r = holes + kv_block_before((uint32_t)__popcll(hole), &all);
         holes += all;
-        for (; hole; hole &= hole - 1) x.target[r++] = page + __builtin_ctzll(hole);
-        r = movers + kv_block_before((int32_t)__popcll(move), &all);
+        kv_each_bit(hole, w, r, [&](uint32_t rank, int32_t p) { x.target[rank] = p; });
+        r = movers + kv_block_before((uint32_t)__popcll(move), &all);
         movers += all;
-        for (; move; move &= move - 1) x.from[r++] = page + __builtin_ctzll(move);
+        kv_each_bit(move, w, r, [&](uint32_t rank, int32_t p) { x.from[rank] = p; });
     }
     __syncthreads();
-    const int32_t n = min(holes, movers);  // equal, unless the free bits are not the counts'
+    const int32_t n = (int32_t)min(holes, movers);  // equal, unless the free bits are not the counts'
     for (int32_t k = tid; k < n; k += kKvPlanThreads) {
         const int32_t p = x.from[k], q = x.target[k];
         x.to[p] = q;
@@ -518,24 +664,24 @@ __global__ void __launch_bounds__(256) kv_compact_move_kernel(KvCompact x, int32
 // ---- attention's split of large batches --------------------------------------------------
 __global__ void __launch_bounds__(kKvPlanThreads) kv_plan_kernel(KvAttend a) {
     const int tid = (int)threadIdx.x;
-    int64_t mine = 0, total = 0;  // blocks
+    uint32_t mine = 0, total = 0;  // blocks
     auto span = [&](int64_t i) {
         const int32_t s = a.slots[i];
         return kv_span(kv_slot_ok(a.c, s) ? kv_length(a.c, s) : 0, a.window);
     };
-    for (int64_t i = tid; i < a.n; i += kKvPlanThreads) mine += kv_blocks(span(i));
+    for (int64_t i = tid; i < a.n; i += kKvPlanThreads) mine = kv_add(mine, (uint32_t)kv_blocks(span(i)));
     kv_block_before(mine, &total);
-    const int32_t chunk = kv_chunk_tokens((int32_t)min(total, (int64_t)INT32_MAX / (kKvBlock / kKvStep)), a.split);
-    int32_t before = 0;
+    const uint32_t most = INT32_MAX / (kKvBlock / kKvStep);
+    const int32_t chunk = kv_chunk_tokens((int32_t)min(total, most), a.split);
+    uint32_t before = 0;
     for (int64_t i0 = 0; i0 < a.n; i0 += kKvPlanThreads) {
         const int64_t i = i0 + tid;
-        const int32_t cnt = i < a.n ? kv_chunks(span(i), chunk) : 0;
-        int32_t all = 0;
-        const int32_t at = before + kv_block_before(cnt, &all);
-        if (i < a.n) a.plan[i] = at;
+        uint32_t all = 0;
+        const uint32_t at = before + kv_block_before(i < a.n ? (uint32_t)kv_chunks(span(i), chunk) : 0, &all);
+        if (i < a.n) a.plan[i] = (int32_t)at;
         before += all;
     }
-    if (tid == 0) a.plan[a.n] = before;
+    if (tid == 0) a.plan[a.n] = (int32_t)before;
 }
 
 }  // namespace pr

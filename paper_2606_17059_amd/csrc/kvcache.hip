@@ -43,6 +43,7 @@ class DeviceScope {
 };
 
 constexpr int64_t kMostGrid = ((int64_t)1 << 32) / 256 - 1;  // workgroups of 256 threads in a launch
+constexpr int64_t kMostEntries = ((int64_t)1 << 32) / pr::kKvPageThreads - 2;  // of a fork or trim, a workgroup each
 constexpr int64_t kMostRows = INT32_MAX;
 
 int element_bytes(const pr_kv *c) { return c->dtype == PR_KV_E4M3 ? 1 : 2; }
@@ -131,6 +132,20 @@ int64_t extend_parts(const pr_kv *c, int64_t n, int64_t rows, void *work, pr::Kv
     x->fresh = p.take<int32_t>(x->most);
     x->copies = p.take<int32_t>(n);
     x->count = p.take<int32_t>(2);
+    return p.bytes;
+}
+
+// A fork or trim whose tables have this many pages changes them in a second launch,
+// if its grid can be had.
+dim3 column_grid(const pr_kv *c, int64_t n) {
+    return dim3((unsigned)((c->slot_pages + 63) / 64), (unsigned)((n + pr::kKvSharedEntries - 1) / pr::kKvSharedEntries));
+}
+
+int64_t change_parts(const pr_kv *c, int64_t n, void *work, pr::KvChange *x) {
+    const dim3 grid = column_grid(c, n);
+    if (n < 16 || n * c->slot_pages < pr::kKvShared || grid.y > 65535 || grid.x > kMostEntries) return 0;
+    Parts p(work);
+    x->columns = p.take<int2>(n);
     return p.bytes;
 }
 
@@ -229,6 +244,10 @@ pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, in
         if (n * m > kMostGrid) return fail(PR_EINVAL, "the batch has too many entries and query heads");
         pr::KvAttend a;
         *bytes = attend_parts(c, n, (int32_t)m, 0, nullptr, &a);
+    } else if (call == PR_KV_WORK_CHANGE) {
+        if (n > kMostEntries) return fail(PR_EINVAL, "n is past 2^22 - 2");
+        pr::KvChange x;
+        *bytes = change_parts(c, n, nullptr, &x);
     } else if (call == PR_KV_WORK_COMPACT) {
         pr::KvCompact x;
         *bytes = compact_parts(c, nullptr, &x);
@@ -261,10 +280,11 @@ pr_status pr_kv_extend(const pr_kv *c, const int32_t *slots, const int64_t *offs
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return launched(e, "pr_kv_extend");
     // a thread a row or new page; a wave a copied page's (layer, head, keys or values)
-    const int64_t copies = std::min<int64_t>(n * c->layers * c->kv_heads * 2, 4096) * 64;
-    const unsigned grid = blocks(std::max({rows, x.most, copies}), 65536);
-    if (c->dtype == PR_KV_E4M3) pr::kv_extend_place_kernel<uint8_t><<<grid, 256, 0, st>>>(x);
-    else pr::kv_extend_place_kernel<uint16_t><<<grid, 256, 0, st>>>(x);
+    const unsigned row_blocks = blocks(std::max(rows, x.most), 8192);
+    const int64_t copies = std::min<int64_t>(n * c->layers, 1 << 20) * c->kv_heads * 2;
+    const unsigned grid = row_blocks + (n > 0 ? (unsigned)std::min<int64_t>((copies + 3) / 4, 1024) : 0);
+    if (c->dtype == PR_KV_E4M3) pr::kv_extend_place_kernel<uint8_t><<<grid, 256, 0, st>>>(x, row_blocks);
+    else pr::kv_extend_place_kernel<uint16_t><<<grid, 256, 0, st>>>(x, row_blocks);
     return launched(hipGetLastError(), "pr_kv_extend");
 }
 
@@ -284,7 +304,7 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
     const bool aligned = !((((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) || (rows > 1 && (k_stride | v_stride) & 7));
     const pr::KvRows x{view(c), place, k_rows, v_rows, k_stride, v_stride, rows, layer, aligned};
     hipStream_t st = (hipStream_t)hip_stream;
-    const unsigned grid = blocks((rows + 3) / 4 * 4 * (width / 8), kMostGrid);
+    const unsigned grid = (blocks((rows + 7) / 8 * 8 * (width / 8), kMostGrid - 7) + 7) / 8 * 8;
     if (c->dtype != PR_KV_E4M3) pr::kv_write_kernel<pr::KvSame><<<grid, 256, 0, st>>>(x);
     else if (io == PR_KV_BF16) pr::kv_write_kernel<pr::KvE4m3<true>><<<grid, 256, 0, st>>>(x);
     else pr::kv_write_kernel<pr::KvE4m3<false>><<<grid, 256, 0, st>>>(x);
@@ -337,28 +357,46 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
 }
 
 pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
-                     void *hip_stream) {
+                     void *workspace, int64_t workspace_bytes, void *hip_stream) {
     if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
-    if (n < 0 || n > kMostGrid) return fail(PR_EINVAL, "n is negative or past 2^24 - 2");
+    if (n < 0 || n > kMostEntries) return fail(PR_EINVAL, "n is negative or past 2^22 - 2");
     if (n == 0) return ok();
     if (!src || !dst || !tokens) return fail(PR_EINVAL, "NULL device pointer");
+    pr::KvChange x{view(c), src, dst, tokens, 1, n, nullptr};
+    if (const char *w = wrong_work(workspace, workspace_bytes, change_parts(c, n, workspace, &x)))
+        return fail(PR_EINVAL, w);
     DeviceScope ds(c->device);
     if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
-    pr::kv_fork_kernel<<<(unsigned)n, 256, 0, (hipStream_t)hip_stream>>>(view(c), src, dst, tokens, n);
-    return launched(hipGetLastError(), "pr_kv_fork");
+    hipStream_t st = (hipStream_t)hip_stream;
+    pr::kv_fork_kernel<<<(unsigned)n, pr::kKvPageThreads, 0, st>>>(x);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && x.columns) {
+        pr::kv_change_columns_kernel<true><<<column_grid(c, n), pr::kKvPageThreads, 0, st>>>(x);
+        e = hipGetLastError();
+    }
+    return launched(e, "pr_kv_fork");
 }
 
 pr_status pr_kv_trim(const pr_kv *c, const int32_t *slots, const int32_t *keep, int64_t keep_stride, int64_t n,
-                     void *hip_stream) {
+                     void *workspace, int64_t workspace_bytes, void *hip_stream) {
     if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
-    if (n < 0 || n > kMostGrid) return fail(PR_EINVAL, "n is negative or past 2^24 - 2");
+    if (n < 0 || n > kMostEntries) return fail(PR_EINVAL, "n is negative or past 2^22 - 2");
     if (keep && keep_stride < 0) return fail(PR_EINVAL, "keep_stride is negative");
     if (n == 0) return ok();
     if (!slots) return fail(PR_EINVAL, "NULL device pointer");
+    pr::KvChange x{view(c), nullptr, slots, keep, keep_stride, n, nullptr};
+    if (const char *w = wrong_work(workspace, workspace_bytes, change_parts(c, n, workspace, &x)))
+        return fail(PR_EINVAL, w);
     DeviceScope ds(c->device);
     if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
-    pr::kv_trim_kernel<<<(unsigned)n, 256, 0, (hipStream_t)hip_stream>>>(view(c), slots, keep, keep_stride);
-    return launched(hipGetLastError(), "pr_kv_trim");
+    hipStream_t st = (hipStream_t)hip_stream;
+    pr::kv_trim_kernel<<<(unsigned)n, pr::kKvPageThreads, 0, st>>>(x);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && x.columns) {
+        pr::kv_change_columns_kernel<false><<<column_grid(c, n), pr::kKvPageThreads, 0, st>>>(x);
+        e = hipGetLastError();
+    }
+    return launched(e, "pr_kv_trim");
 }
 
 pr_status pr_kv_compact(const pr_kv *c, int32_t *moved, void *workspace, int64_t workspace_bytes,

@@ -15,7 +15,7 @@ from typing import Optional
 from .router import PR_OK, KvDescription, _check, _dev, _load_torch, _stream_ptr, lib
 
 PR_KV_BF16, PR_KV_F16, PR_KV_E4M3 = 0, 1, 2
-PR_KV_WORK_EXTEND, PR_KV_WORK_ATTEND, PR_KV_WORK_COMPACT = 0, 1, 2
+PR_KV_WORK_EXTEND, PR_KV_WORK_ATTEND, PR_KV_WORK_COMPACT, PR_KV_WORK_CHANGE = 0, 1, 2, 3
 
 
 class KVCache:
@@ -74,7 +74,7 @@ class KVCache:
             self.k_scale, self.v_scale, k.data_ptr() or None, v.data_ptr() or None, *strides, table.data_ptr() or None, lengths.data_ptr() or None, refs.data_ptr() or None,
             free.data_ptr() or None, skipped.data_ptr())
         self._ref = ctypes.byref(self._desc)
-        self._index, self._int32, self._int64 = k.device.index, torch.int32, torch.int64
+        self._index, self._int32, self._int64, self._uint8 = k.device.index, torch.int32, torch.int64, torch.uint8
         # types that rows of new tokens and queries may have
         self._io = {torch.bfloat16: PR_KV_BF16, torch.float16: PR_KV_F16} if k.dtype.itemsize == 1 else \
             {k.dtype: codes[k.dtype]}
@@ -121,6 +121,14 @@ class KVCache:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _work(self, call: int, n: int, m: int, stream):
+        """(a workspace or None, its address, its size)."""
+        size = self._work_bytes(call, n, m)
+        if not size:
+            return None, None, 0
+        work = self._empty((size,), self._uint8, stream)
+        return work, work.data_ptr(), size
 
     def _st(self, stream) -> int:
         if stream is not None and stream.device != self.device:
@@ -173,10 +181,9 @@ class KVCache:
             place = self._empty((rows,), self._int32, stream)
         else:
             self._ints(place, self._int32, "place", rows)
-        size = self._work_bytes(PR_KV_WORK_EXTEND, n, rows)
-        work = self._empty((size,), _load_torch().uint8, stream)
+        work, at, size = self._work(PR_KV_WORK_EXTEND, n, rows, stream)
         s = self._lib.pr_kv_extend(self._ref, slots.data_ptr() or None, offsets.data_ptr(), n, rows,
-                                   place.data_ptr() or None, work.data_ptr() or None, size, st)
+                                   place.data_ptr() or None, at, size, st)
         if s != PR_OK:
             _check(s)
         return place
@@ -212,12 +219,11 @@ class KVCache:
             _dev(lse, torch.float32, "lse")
             if tuple(lse.shape) != (n, heads) or lse.device != self.device:
                 raise ValueError("lse must be [n, heads] on the cache's device")
-        size = self._work_bytes(PR_KV_WORK_ATTEND, n, heads)
-        work = self._empty((size,), torch.uint8, stream) if size else None
+        work, at, size = self._work(PR_KV_WORK_ATTEND, n, heads, stream)
         s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, stride,
                                    heads, io, self._scale if scale is None else scale, window,
                                    out.data_ptr() or None, lse.data_ptr() or None if lse is not None else None,
-                                   work.data_ptr() if work is not None else None, size, st)
+                                   at, size, st)
         if s != PR_OK:
             _check(s)
         return out
@@ -227,8 +233,10 @@ class KVCache:
         n = self._ints(src, self._int32, "src")
         self._ints(dst, self._int32, "dst", n)
         self._ints(tokens, self._int32, "tokens", n)
+        st = self._st(stream)
+        work, at, size = self._work(PR_KV_WORK_CHANGE, n, 0, stream)
         s = self._lib.pr_kv_fork(self._ref, src.data_ptr() or None, dst.data_ptr() or None,
-                                 tokens.data_ptr() or None, n, self._st(stream))
+                                 tokens.data_ptr() or None, n, at, size, st)
         if s != PR_OK:
             _check(s)
 
@@ -244,20 +252,20 @@ class KVCache:
             if keep.device != self.device or tuple(keep.shape) != (n,):
                 raise ValueError(f"keep must be [{n}] on the cache's device")
             stride = keep.stride(0)
+        st = self._st(stream)
+        work, at, size = self._work(PR_KV_WORK_CHANGE, n, 0, stream)
         s = self._lib.pr_kv_trim(self._ref, slots.data_ptr() or None,
-                                 (keep.data_ptr() or None) if keep is not None else None, stride, n, self._st(stream))
+                                 (keep.data_ptr() or None) if keep is not None else None, stride, n, at, size, st)
         if s != PR_OK:
             _check(s)
 
     def compact(self, stream=None):
         """Move the held pages to the lowest ids; returns int32 [2] on the device: pages moved, pages held
         (pr_kv_compact)."""
-        torch = _load_torch()
         st = self._st(stream)
-        size = self._work_bytes(PR_KV_WORK_COMPACT, 0, 0)
-        moved = self._empty((2,), torch.int32, stream)
-        work = self._empty((size,), torch.uint8, stream)
-        s = self._lib.pr_kv_compact(self._ref, moved.data_ptr(), work.data_ptr(), size, st)
+        moved = self._empty((2,), self._int32, stream)
+        work, at, size = self._work(PR_KV_WORK_COMPACT, 0, 0, stream)
+        s = self._lib.pr_kv_compact(self._ref, moved.data_ptr(), at, size, st)
         if s != PR_OK:
             _check(s)
         return moved

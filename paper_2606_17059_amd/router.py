@@ -132,8 +132,8 @@ def lib() -> ctypes.CDLL:
                        ("pr_kv_write", [kv, i32, _vp, _vp, i64, _vp, i64, i64, i32, _vp]),
                        ("pr_kv_attend", [kv, i32, _vp, i64, _vp, i64, i32, i32, ctypes.c_float, i32, _vp, _vp, _vp,
                                          i64, _vp]),
-                       ("pr_kv_fork", [kv, _vp, _vp, _vp, i64, _vp]),
-                       ("pr_kv_trim", [kv, _vp, _vp, i64, i64, _vp]),
+                       ("pr_kv_fork", [kv, _vp, _vp, _vp, i64, _vp, i64, _vp]),
+                       ("pr_kv_trim", [kv, _vp, _vp, i64, i64, _vp, i64, _vp]),
                        ("pr_kv_compact", [kv, _vp, _vp, i64, _vp]),
                        ("pr_kv_check", [kv, _vp])):
         getattr(L, name).argtypes = args

@@ -468,6 +468,48 @@ def test_random_calls_match_the_model(seed, page, pages, slots, slot_pages, batc
     _content_same(c, m, range(slots), "end")
 
 
+@pytest.mark.parametrize("n,slot_pages,parents", [(40, 4000, 3), (600, 700, 5), (1100, 130, 40)])
+def test_large_forks_and_trims(n, slot_pages, parents):
+    """Batches whose tables have many pages: counts that forks of one sequence change together, more sequences than
+    a column has places for, entries past a workgroup's, and entries that are skipped among them."""
+    import torch
+    announce(f"fork and trim {n} entries of {parents} sequences")
+    rng = np.random.default_rng(n)
+    T, slots = 16, parents + n + 3
+    held = rng.integers(slot_pages * T // 2, slot_pages * T, parents).tolist()
+    P = sum(-(-x // T) for x in held) + 2 * n
+    c = _cache(1, 1, 64, T, P, slots, slot_pages)
+    m = kv_model.Pages(T, P, slots, slot_pages)
+    junk = rng.permutation(slots)[:parents].tolist()  # scattered pages: some are taken and given back first
+    for k in range(2):
+        off = [0] + np.cumsum(held).tolist()
+        s = junk if k == 0 else list(range(parents))
+        assert c.extend(_ints(s), _t(off, torch.int64), off[-1]).tolist() == m.extend(s, off, off[-1])
+        if k == 0:
+            c.trim(_ints(s))
+            m.trim(s, [0] * parents)
+    src = rng.integers(0, parents, n).tolist()
+    dst = list(range(parents, parents + n))
+    tokens = [int(rng.integers(0, held[a] + 1)) for a in src]
+    tokens[3], dst[5], src[7], dst[9], dst[11] = held[src[3]] + 1, -1, slots, dst[8], src[11]
+    c.fork(_ints(src), _ints(dst), _ints(tokens))
+    m.fork(src, dst, tokens)
+    _same(c, m, "fork")
+    assert int(c.skipped) == m.skipped >= 4
+    s = rng.integers(-1, slots + 1, n).tolist()
+    keep = rng.integers(-1, slot_pages * T, n).tolist()
+    c.trim(_ints(s), _ints(keep))
+    m.trim(s, keep)
+    _same(c, m, "trim")
+    c.extend(_ints(dst[:5]), _offsets([1] * 5), 5)
+    m.extend(dst[:5], list(range(6)), 5)
+    _same(c, m, "extend")
+    c.trim(_ints(list(range(slots))))
+    m.trim(list(range(slots)), [0] * slots)
+    _same(c, m, "all")
+    assert not any(m.refs) and int(c.skipped) == m.skipped
+
+
 @pytest.mark.parametrize("n", [1023, 1024, 1025, 2500])
 def test_extend_batches_past_a_workgroup(n):
     """More entries than the planning workgroup has threads, more pages than it has words at a time."""

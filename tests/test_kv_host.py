@@ -33,8 +33,8 @@ def _calls(d, n=3, rows=5, work=FAKE, size=1 << 30):
         "pr_kv_extend": [r, FAKE, FAKE, n, rows, FAKE, work, size, None],
         "pr_kv_write": [r, 0, FAKE, FAKE, 128, FAKE, 128, rows, 0, None],
         "pr_kv_attend": [r, 0, FAKE, n, FAKE, 4 * 64, 4, 0, 0.125, 0, FAKE, None, work, size, None],
-        "pr_kv_fork": [r, FAKE, FAKE, FAKE, n, None],
-        "pr_kv_trim": [r, FAKE, FAKE, 1, n, None],
+        "pr_kv_fork": [r, FAKE, FAKE, FAKE, n, work, size, None],
+        "pr_kv_trim": [r, FAKE, FAKE, 1, n, work, size, None],
         "pr_kv_compact": [r, None, work, size, None],
         "pr_kv_check": [r, None],
     }
@@ -71,7 +71,7 @@ def test_the_binding_lays_out_the_description_as_the_header():
 
 
 BAD = [  # call, index of an argument, a value it refuses
-    ("pr_kv_workspace", 1, 3), ("pr_kv_workspace", 2, -1), ("pr_kv_workspace", 3, 1 << 31),
+    ("pr_kv_workspace", 1, 4), ("pr_kv_workspace", 2, -1), ("pr_kv_workspace", 3, 1 << 31),
     ("pr_kv_workspace", 4, None),
     ("pr_kv_extend", 1, None), ("pr_kv_extend", 2, None), ("pr_kv_extend", 3, -1), ("pr_kv_extend", 4, -1),
     ("pr_kv_extend", 3, 1 << 31), ("pr_kv_extend", 4, 1 << 31), ("pr_kv_extend", 5, None), ("pr_kv_extend", 6, None),
@@ -85,8 +85,8 @@ BAD = [  # call, index of an argument, a value it refuses
     ("pr_kv_attend", 8, float("inf")), ("pr_kv_attend", 9, -1), ("pr_kv_attend", 10, None),
     ("pr_kv_attend", 10, FAKE + 8),
     ("pr_kv_fork", 1, None), ("pr_kv_fork", 2, None), ("pr_kv_fork", 3, None), ("pr_kv_fork", 4, -1),
-    ("pr_kv_fork", 4, 1 << 24),
-    ("pr_kv_trim", 1, None), ("pr_kv_trim", 3, -1), ("pr_kv_trim", 4, -1), ("pr_kv_trim", 4, 1 << 24),
+    ("pr_kv_fork", 4, 1 << 22),
+    ("pr_kv_trim", 1, None), ("pr_kv_trim", 3, -1), ("pr_kv_trim", 4, -1), ("pr_kv_trim", 4, 1 << 22),
     ("pr_kv_compact", 2, None), ("pr_kv_compact", 2, FAKE + 4), ("pr_kv_compact", 3, 16),
 ]
 
@@ -114,6 +114,19 @@ def test_an_attention_that_splits_wants_its_workspace():
     assert L.pr_kv_workspace(ctypes.byref(_desc()), 1, 3, 5, ctypes.byref(need)) == R.PR_EINVAL  # 5 heads over 2
 
 
+def test_large_forks_and_trims_want_their_workspace():
+    from paper_2606_17059_amd import router as R
+    L, need, d = R.lib(), ctypes.c_int64(0), _desc(slot_pages=1 << 12, num_slots=100)
+    for n, large in ((15, False), (31, False), (32, True)):
+        assert L.pr_kv_workspace(ctypes.byref(d), 3, n, 0, ctypes.byref(need)) == R.PR_OK
+        assert (need.value > 0) == large
+    for work, size in ((None, need.value), (FAKE, need.value - 1), (FAKE + 8, need.value)):
+        calls = _calls(d, n=32, work=work, size=size)
+        for name in ("pr_kv_fork", "pr_kv_trim"):
+            assert getattr(L, name)(*calls[name]) == R.PR_EINVAL
+    assert L.pr_kv_workspace(ctypes.byref(d), 3, 1 << 22, 0, ctypes.byref(need)) == R.PR_EINVAL
+
+
 def test_empty_batches_do_nothing():
     """Zero entries need no pointers and no GPU."""
     from paper_2606_17059_amd import router as R
@@ -122,8 +135,8 @@ def test_empty_batches_do_nothing():
     assert L.pr_kv_extend(r, None, None, 0, 0, None, None, 0, None) == R.PR_OK
     assert L.pr_kv_write(r, 0, None, None, 0, None, 0, 0, 0, None) == R.PR_OK
     assert L.pr_kv_attend(r, 0, None, 0, None, 0, 4, 0, 1.0, 0, None, None, None, 0, None) == R.PR_OK
-    assert L.pr_kv_fork(r, None, None, None, 0, None) == R.PR_OK
-    assert L.pr_kv_trim(r, None, None, 0, 0, None) == R.PR_OK
+    assert L.pr_kv_fork(r, None, None, None, 0, None, 0, None) == R.PR_OK
+    assert L.pr_kv_trim(r, None, None, 0, 0, None, 0, None) == R.PR_OK
 
 
 def test_the_binding_takes_device_tensors_only():
