@@ -44,17 +44,39 @@ __device__ inline uint32_t kv_block_before(uint32_t v, uint32_t *all) {
     return kv_add(before, upto - v);  // exact in the wave unless past everything
 }
 
-// Calls put(rank, page) for the set bits of the wave's 64 words: `bits` is a lane's word,
-// 64 * word its first page and `rank` the number of set bits in the words before.
+// Calls put(rank, page) for the set bits of the workgroup's words, a wave a word: `bits`
+// is a thread's word, 64 * first the first thread's first page, `rank` the number of
+// set bits in the words before its own.  All threads call it with the same number of
+// `words` that may have bits.
 template <typename Put>
-__device__ inline void kv_each_bit(unsigned long long bits, int32_t word, uint32_t rank, Put put) {
-    const int lane = (int)(threadIdx.x & 63);
-    for (uint64_t some = __ballot(bits != 0); some; some &= some - 1) {
-        const int src = __builtin_ctzll(some);
-        const uint64_t w = readlane64(bits, src);
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)rank, src);
-        if (w >> lane & 1)
-            put(first + (uint32_t)__popcll(w & ((1ull << lane) - 1)), 64 * __builtin_amdgcn_readlane(word, src) + lane);
+__device__ inline void kv_each_bit(unsigned long long bits, int32_t first, uint32_t rank, int32_t words, Put put) {
+    const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
+    auto one = [&](uint64_t w, int k, uint32_t r) {
+        if (w >> lane & 1) put(r + (uint32_t)__popcll(w & ((1ull << lane) - 1)), 64 * (first + k) + lane);
+    };
+    const uint64_t some = __ballot(bits != 0);
+    if (words <= 64) {
+        // a wave its own words: dealing them out costs 0.8 us, one wave's 64 words 3 us
+        for (uint64_t m = some; m; m &= m - 1) {
+            const int src = __builtin_ctzll(m);
+            one(readlane64(bits, src), 64 * wave + src, (uint32_t)__builtin_amdgcn_readlane((int)rank, src));
+        }
+        return;
+    }
+    __shared__ unsigned long long word[kKvPlanThreads];
+    __shared__ uint32_t before[kKvPlanThreads];
+    __shared__ uint64_t any[kKvPlanThreads / 64];
+    __syncthreads();  // the arrays are the last call's until here
+    word[threadIdx.x] = bits;
+    before[threadIdx.x] = rank;
+    if (lane == 0) any[wave] = some;
+    __syncthreads();
+    for (int v = 0; v < kKvPlanThreads / 64; ++v) {
+        // of the words of wave v this wave takes every sixteenth
+        for (uint64_t m = any[v] & (0x0001000100010001ull << wave); m; m &= m - 1) {
+            const int k = 64 * v + __builtin_ctzll(m);
+            one(word[k], k, before[k]);
+        }
     }
 }
 
@@ -203,7 +225,7 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_extend_plan_kernel(KvExtend
             unsigned long long left = bits;
             for (uint32_t k = r; k < wanted; ++k, left &= left - 1) taken |= left & (~left + 1);
         }
-        kv_each_bit(taken, w, r, [&](uint32_t rank, int32_t p) {
+        kv_each_bit(taken, f, r, min(words, (int32_t)wanted), [&](uint32_t rank, int32_t p) {
             x.fresh[rank] = p;
             c.refs[p] = 1;
         });
@@ -392,24 +414,24 @@ __device__ inline void kv_write_eight(const KvRows &x, int64_t r, int32_t dim) {
         V8 v;
     } one;
     const KvView &c = x.c;
-    const int32_t p = kv_place(x, r);
+    uint16_t in[8];
+    const int32_t p = kv_place(x, r), q = p & 3;
     if (p < 0) return;
+    kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, in);
     const int32_t head = (int32_t)((uint32_t)dim / (uint32_t)c.head_dim), d = dim - head * c.head_dim;
     const int32_t t = p & (kv_page_tokens(c) - 1);
-    const int64_t page = p >> c.page_shift, lead = r - (p & 3);
+    const int64_t page = p >> c.page_shift, lead = r - q;
     const uint16_t *vrow = (const uint16_t *)x.v + dim;
-    uint16_t in[8];
     bool whole = true;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) whole &= kv_place(x, lead + e) == (p & ~3) + e;
+    for (int e = 0; e < 4; ++e) whole &= kv_place(x, lead + e) == p - q + e;
 
-    kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, in);
     P::put(in, c.k_scale, one.e);
     *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = one.v;
 
     T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
     if (whole) {
-        const int32_t two = 2 * (p & 3);
+        const int32_t two = 2 * q;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint16_t *src = vrow + (lead + e) * x.v_stride + two;
@@ -423,7 +445,7 @@ __device__ inline void kv_write_eight(const KvRows &x, int64_t r, int32_t dim) {
         kv_load8(vrow + r * x.v_stride, x.aligned, in);
         P::put(in, c.v_scale, one.e);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dst[4 * i + (p & 3)] = one.e[i];
+        for (int i = 0; i < 8; ++i) dst[4 * i + q] = one.e[i];
     }
 }
 
@@ -451,7 +473,7 @@ __global__ void __launch_bounds__(256) kv_write_kernel(KvRows x) {
 // nanosecond at best: 24 us; joined, 9,000 are left.)
 constexpr int kKvPageThreads = 1024, kKvPageTurn = 4;
 constexpr int64_t kKvShared = 1 << 17;  // pages of a batch's tables from which there is a second launch
-constexpr int kKvSharedEntries = 512;   // entries of one of its workgroups
+constexpr int kKvSharedEntries = 64;    // entries of one of its workgroups: four a wave, on their way at once
 
 struct KvChange {
     KvView c;
@@ -528,51 +550,52 @@ __global__ void __launch_bounds__(kKvPageThreads) kv_trim_kernel(KvChange x) {
     else kv_change_row<false>(x, i, 0, 0);
 }
 
-// 64 columns of up to kKvSharedEntries entries' table rows: a lane a column, a wave
-// every sixteenth entry.  A column has places for the counts of 16 pages; what finds
-// none is changed by itself.
+// 64 columns of kKvSharedEntries entries' table rows: a lane a column, a wave every
+// sixteenth entry.  A column has places for the counts of 16 pages; what finds none is
+// changed by itself.
 template <bool FORK>
 __global__ void __launch_bounds__(kKvPageThreads) kv_change_columns_kernel(KvChange x) {
-    constexpr int PLACES = 16, WAVES = kKvPageThreads / 64;
+    constexpr int PLACES = 16, WAVES = kKvPageThreads / 64, EACH = kKvSharedEntries / WAVES;
     const KvView &c = x.c;
     __shared__ int32_t page[PLACES][64], count[PLACES][64];
+    __shared__ int2 columns[kKvSharedEntries];
+    __shared__ int32_t to[kKvSharedEntries], from[kKvSharedEntries];
     const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
+    const int64_t first = (int64_t)blockIdx.y * kKvSharedEntries;
+    if (threadIdx.x < kKvSharedEntries) {
+        const int64_t i = first + threadIdx.x;
+        columns[threadIdx.x] = i < x.n ? x.columns[i] : make_int2(0, 0);
+        to[threadIdx.x] = i < x.n ? x.dst[i] : -1;
+        from[threadIdx.x] = FORK && i < x.n ? x.src[i] : -1;
+    }
     page[wave][lane] = -1;
     count[wave][lane] = 0;
     __syncthreads();
     const int32_t col = (int32_t)blockIdx.x * 64 + lane;
-    const int64_t first = (int64_t)blockIdx.y * kKvSharedEntries, last = min(x.n, first + kKvSharedEntries);
     auto change = [&](int32_t p, int32_t by) {
         if (FORK) atomicAdd(&c.refs[p], by);
         else if (atomicSub(&c.refs[p], by) == by) atomicOr(&c.free_pages[p >> 6], 1ull << (p & 63));
     };
-    for (int64_t i0 = first + wave; i0 < last; i0 += WAVES * kKvPageTurn) {
-        int32_t p[kKvPageTurn];
-        int32_t *at[kKvPageTurn];
+    int32_t p[EACH];
+    bool in[EACH];
 #pragma unroll
-        for (int e = 0; e < kKvPageTurn; ++e) {
-            const int64_t i = i0 + e * WAVES;
-            const int2 r = i < last ? x.columns[i] : make_int2(0, 0);
-            p[e] = -1;
-            at[e] = nullptr;
-            if (col >= r.x && col < r.y) {
-                at[e] = c.table + (int64_t)x.dst[i] * c.slot_pages + col;
-                p[e] = FORK ? c.table[(int64_t)x.src[i] * c.slot_pages + col] : *at[e];
-            }
-        }
+    for (int e = 0; e < EACH; ++e) {
+        const int i = wave + e * WAVES;
+        in[e] = col >= columns[i].x && col < columns[i].y;
+        p[e] = in[e] ? c.table[(int64_t)(FORK ? from : to)[i] * c.slot_pages + col] : -1;
+    }
 #pragma unroll
-        for (int e = 0; e < kKvPageTurn; ++e) {
-            if (!at[e]) continue;
-            *at[e] = FORK ? p[e] : -1;
-            if (!kv_page_ok(c, p[e])) continue;
-            int32_t *key = &page[p[e] & (PLACES - 1)][lane];
-            const int32_t was = atomicCAS(key, -1, p[e]);
-            if (was == -1 || was == p[e]) atomicAdd(&count[p[e] & (PLACES - 1)][lane], 1);
-            else change(p[e], 1);
-        }
+    for (int e = 0; e < EACH; ++e) {
+        if (!in[e]) continue;
+        c.table[(int64_t)to[wave + e * WAVES] * c.slot_pages + col] = FORK ? p[e] : -1;
+        if (!kv_page_ok(c, p[e])) continue;
+        const int at = p[e] & (PLACES - 1);
+        const int32_t was = atomicCAS(&page[at][lane], -1, p[e]);
+        if (was == -1 || was == p[e]) atomicAdd(&count[at][lane], 1);
+        else change(p[e], 1);
     }
     __syncthreads();
-    static_assert(PLACES == WAVES, "a thread a place");
+    static_assert(PLACES == WAVES && EACH * WAVES == kKvSharedEntries, "a thread a place, all entries dealt");
     if (count[wave][lane]) change(page[wave][lane], count[wave][lane]);
 }
 
@@ -608,10 +631,10 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_compact_plan_kernel(KvCompa
         uint32_t all = 0;
         uint32_t r = holes + kv_block_before((uint32_t)__popcll(hole), &all);
         holes += all;
-        kv_each_bit(hole, w, r, [&](uint32_t rank, int32_t p) { x.target[rank] = p; });
+        kv_each_bit(hole, w0, r, words, [&](uint32_t rank, int32_t p) { x.target[rank] = p; });
         r = movers + kv_block_before((uint32_t)__popcll(move), &all);
         movers += all;
-        kv_each_bit(move, w, r, [&](uint32_t rank, int32_t p) { x.from[rank] = p; });
+        kv_each_bit(move, w0, r, words, [&](uint32_t rank, int32_t p) { x.from[rank] = p; });
     }
     __syncthreads();
     const int32_t n = (int32_t)min(holes, movers);  // equal, unless the free bits are not the counts'
