@@ -8,3 +8,4 @@ from .router import (Forest, RouterError, pr_forest_check, pr_forest_create,  # 
                      pr_route_noalloc, pr_route_select, pr_tree_tokens, pr_forest_compact, pr_set_local_peer, pr_set_time, pr_touch, pr_evict_lru, eligible_words,
                      PR_SELECT_PREFER_LOCAL)
 from .kvcache import KVCache  # noqa: F401
+from .node_cache import Admission, NodeCache  # noqa: F401

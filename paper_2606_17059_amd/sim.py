@@ -27,6 +27,13 @@ routing node's estimate of it ("expected"), as fractions of the prompt.
 The routing itself is the library's; the simulator only drives it through a
 backend (RouterBackend below), so that the same trace can be replayed against
 another implementation of the calls.
+
+With a CacheConfig a node also has the KV cache whose index its own tree is
+(node_cache.py): a request is admitted to it as a fork of its longest cached
+prefix, keys and values of the other tokens are written on every layer, its last
+token attends to all of them (the paper's workload has one output token), and
+the cached sequences follow the tree's evictions.  There is no model: keys, values
+and queries come from fixed random tables by token and position.
 """
 from __future__ import annotations
 
@@ -58,16 +65,88 @@ class SimConfig:
     seed: int = 20261202
 
 
-class RouterBackend:
-    """One node's router: the calls the simulation makes, on the library."""
+@dataclass
+class CacheConfig:
+    """A node's KV cache; the heads are those of the paper's 0.5B model."""
+    layers: int = 4
+    kv_heads: int = 2
+    q_heads: int = 14
+    head_dim: int = 64
+    page_tokens: int = 16
+    slots: int = 256        # sequences kept at once
+    max_tokens: int = 1024  # of a sequence
+    seed: int = 20261202
 
-    def __init__(self, num_peers: int, local: int, device=None):
+
+class ServedCache:
+    """A node's KV cache in the simulation: it admits requests, writes their rows and takes their last token's
+    attention, rows coming from tables in place of a model."""
+
+    TABLE = 4096
+
+    def __init__(self, forest, local: int, cfg: CacheConfig, kv_tokens: int, device):
+        import torch
+        from .kvcache import KVCache
+        from .node_cache import NodeCache
+        T = cfg.page_tokens
+        # full pages of kv_tokens distinct tokens, and a partly filled one of each sequence
+        pages = -(-kv_tokens // T) + cfg.slots + -(-cfg.max_tokens // T)
+        cache = KVCache.create(cfg.layers, cfg.kv_heads, cfg.head_dim, T, pages, cfg.slots, -(-cfg.max_tokens // T),
+                               torch.bfloat16, device)
+        self.node = NodeCache(forest, local, cache)
+        g = torch.Generator(device=device).manual_seed(cfg.seed)
+        shape = (cfg.layers, self.TABLE, 2, cfg.kv_heads, cfg.head_dim)
+        self.kv = torch.empty(shape, dtype=torch.bfloat16, device=device).normal_(generator=g)
+        self.q = torch.empty((cfg.layers, self.TABLE, cfg.q_heads, cfg.head_dim), dtype=torch.bfloat16,
+                             device=device).normal_(generator=g)
+        self.cached, self.admitted, self.given_up, self.moved = 0, 0, 0, 0
+        self.answer = None  # the last request's attention, [layers, heads, head_dim]
+
+    def row_ids(self, tokens, first: int = 0):
+        """Row of the tables for each token at its position."""
+        t = np.asarray(tokens, np.int64)
+        return (t * 31 + np.arange(first, first + len(t)) * 7) % self.TABLE
+
+    def serve(self, tokens) -> None:
+        import torch
+        a = self.node.admit(tokens)
+        c = self.node.cache
+        ids = torch.from_numpy(self.row_ids(tokens[a.cached:], a.cached)).to(c.device)
+        last = int(self.row_ids(tokens)[-1])
+        slot = torch.tensor([a.slot], dtype=torch.int32, device=c.device)
+        out = []
+        for layer in range(c.layers):
+            rows = self.kv[layer, ids]
+            c.write(layer, a.place, rows[:, 0], rows[:, 1])
+            out.append(c.attend(layer, slot, self.q[layer, last:last + 1])[0])
+        self.answer = torch.stack(out)
+        self.admitted += len(tokens)
+        self.cached += a.cached
+
+    def follow(self) -> None:
+        self.given_up += self.node.follow()
+
+    def compact(self) -> None:
+        self.moved += self.node.compact()[0]
+
+    def close(self) -> None:
+        self.node.cache.check()
+        self.node.close()
+
+
+class RouterBackend:
+    """One node's router: the calls the simulation makes, on the library.  With `cache` (and the node's budget of
+    tokens) it also serves what it inserts into its own tree from a KV cache."""
+
+    def __init__(self, num_peers: int, local: int, device=None, cache: Optional[CacheConfig] = None,
+                 kv_tokens: int = 0):
         import torch
         from .router import Forest
         self.dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
         self.f = Forest(num_peers)
         self.local = local
         self.f.set_local_peer(local)
+        self.cache = ServedCache(self.f, local, cache, kv_tokens, self.dev) if cache is not None else None
 
     def _csr(self, seqs):
         import torch
@@ -94,14 +173,21 @@ class RouterBackend:
         return self.f.tree_tokens(self.local)
 
     def evict(self, n: int) -> int:
-        return self.f.evict_lru(n)
+        ev = self.f.evict_lru(n)
+        if self.cache is not None:
+            self.cache.follow()
+        return ev
 
     def insert(self, peer: int, q) -> None:
         import torch
         t, o = self._csr([q])
         self.f.merge(torch.tensor([peer], dtype=torch.int32, device=self.dev), t, o)
+        if peer == self.local and self.cache is not None:
+            self.cache.serve(q)
 
     def export_local(self):
+        if self.cache is not None:
+            self.cache.compact()
         return self.f.export_snapshot(self.local)
 
     def load_estimate(self, peer: int, snapshot) -> None:
@@ -109,6 +195,8 @@ class RouterBackend:
         self.f.load_snapshot_device(peer, t.contiguous(), o)
 
     def close(self) -> None:
+        if self.cache is not None:
+            self.cache.close()
         self.f.close()
 
 
@@ -240,10 +328,26 @@ def main() -> int:
     ap.add_argument("--kv-tokens", type=int, default=20000)
     ap.add_argument("--no-route", action="store_true")
     ap.add_argument("--seed", type=int, default=20261202)
+    ap.add_argument("--kv-cache", action="store_true",
+                    help="each node serves its requests from a KV cache that follows its tree")
+    ap.add_argument("--kv-slots", type=int, default=256, help="sequences a node's KV cache keeps")
     a = ap.parse_args()
     cfg = SimConfig(nodes=a.nodes, requests=a.requests, skew=a.skew, comm_ms=a.comm_ms, poll_ms=a.poll_ms,
                     kv_tokens=a.kv_tokens, route=not a.no_route, seed=a.seed)
-    out = summarize(simulate(cfg))
+    if a.kv_cache:
+        cache = CacheConfig(slots=a.kv_slots, max_tokens=cfg.prefix_len[1] + cfg.question_len[1], seed=cfg.seed)
+        nodes = [RouterBackend(cfg.nodes, i, cache=cache, kv_tokens=cfg.kv_tokens) for i in range(cfg.nodes)]
+        out = summarize(simulate(cfg, nodes))
+        served = [nd.cache for nd in nodes]
+        out["kv_cached"] = sum(s.cached for s in served) / max(1, sum(s.admitted for s in served))
+        out["kv_given_up"] = sum(s.given_up for s in served)
+        out["kv_pages_moved"] = sum(s.moved for s in served)
+        out["kv_pages_held"] = [int((s.node.cache.refs > 0).sum()) for s in served]
+        out["kv_config"] = asdict(cache)
+        for nd in nodes:
+            nd.close()
+    else:
+        out = summarize(simulate(cfg))
     out["config"] = asdict(cfg)
     print(json.dumps(out))
     return 0
