@@ -545,6 +545,7 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  * counted) give out 0 and lse -infinity.  Tokens of a page whose table entry
  * is out of range are left out.  Sums, maxima and weights are kept in 32 bits.
  * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
+ * n * q_heads is below 2^24 and n * slot_pages * page_tokens below 2^38.
  */
 pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int64_t n, const void *q,
                        int64_t q_stride, int32_t q_heads, int32_t io, float scale, int32_t window, void *out,

@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kv_launch.h"
 #include "kv_layout.h"
 #include "wave_ops.h"
@@ -91,106 +93,131 @@ __device__ __forceinline__ float rows_sum(float x) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Where a workgroup works: an entry (-1: nowhere), and which of its chunks.
-struct KvUnit {
-    int32_t entry, slot, length, chunk, chunks, first_unit, chunk_tokens;
-};
+using Scalar = const __attribute__((address_space(4))) int32_t;  // read by scalar loads
+__device__ __forceinline__ Scalar *scalar(const int32_t *p) { return (Scalar *)(uintptr_t)p; }
 
-// A slot's tokens; none for a slot that is none.
-__device__ __forceinline__ int32_t kv_known_length(const KvView &c, int32_t slot) {
-    return kv_slot_ok(c, slot) ? kv_length(c, slot) : 0;
+// The steps [begin, end) a workgroup takes, `first` of which are before those of the
+// entry it begins with (-1: nothing to take).  Of shares of `size` steps it is number
+// `index`.  Sequences follow each other in the numbering of the steps, or, where
+// shares keep to sequences, each has a numbering of its own (first = index = 0).
+struct KvShare {
+    uint32_t begin, end, size, first, index;
+    int32_t entry;
+};
+__device__ __forceinline__ KvShare kv_share_of(uint32_t u, uint32_t size, uint32_t steps) {
+    KvShare r{u * size, 0, size, 0, u, -1};
+    r.end = min(r.begin + size, steps);
+    return r;
+}
+// Share k of an entry's own.
+__device__ __forceinline__ KvShare kv_own_share(int32_t entry, uint32_t steps, uint32_t shares, uint32_t k) {
+    KvShare r = kv_share_of(k, kv_even(steps, shares), steps);
+    r.index = 0;
+    r.entry = entry;
+    return r;
 }
 
-// Unit u of the batch's chunks in the order of its entries, found by every wave
-// for itself from the lengths (a batch of at most kKvScan entries: E * 64).  A
-// kernel before this one that wrote the same down took longer than the two loads
-// and a dozen lane operations that it saved (see kv_plan_kernel).
+// Share u of a batch of at most E * 64 entries, found by every wave for itself from
+// the lengths.  A kernel before this one that wrote the same down would take longer
+// than the two loads and two dozen lane operations that it saved.
 template <int E>
-__device__ inline KvUnit kv_find_unit(const KvAttend &a, int32_t u) {
+__device__ inline KvShare kv_find_share(const KvAttend &a, uint32_t u) {
     const int lane = (int)(threadIdx.x & 63);
-    int32_t slot[E], length[E], span[E], mine[E], total = 0;
+    int32_t slot[E];
+    uint32_t mine[E], upto[E], total = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) slot[e] = e * 64 + lane < a.n ? a.slots[e * 64 + lane] : -1;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        length[e] = kv_known_length(a.c, slot[e]);
-        span[e] = kv_span(length[e], a.window);
-        total += kv_blocks(span[e]);
+        const int32_t length = kv_slot_ok(a.c, slot[e]) ? kv_length(a.c, slot[e]) : 0;
+        mine[e] = e * 64 + lane < a.n ? kv_steps(kv_span(length, a.window)) : 0;
     }
-    int32_t most = kv_chunk_tokens(__builtin_amdgcn_readlane(lanes_upto(total), 63), a.split);
-    // Chunks that end short may be more than the GPU holds at once: longer ones then,
-    // if that puts all of them into one turn.
-    int tries = a.n < a.split.fill && most <= a.split.worth ? 3 : 0;
-    for (;;) {
-        int32_t units = 0;
+    auto add = [&] {
+        total = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            mine[e] = e * 64 + lane < a.n ? kv_chunks(span[e], most) : 0;
-            units += mine[e];
+            upto[e] = total + (uint32_t)lanes_upto((int32_t)mine[e]);
+            total = (uint32_t)__builtin_amdgcn_readlane((int)upto[e], 63);
         }
-        if (tries-- <= 0) break;
-        units = __builtin_amdgcn_readlane(lanes_upto(units), 63);
-        if (units <= a.split.fill) break;
-        most = kv_longer_chunk(most, units, a.split.fill);
+    };
+    // the entry in whose part of the sums v lies
+    int entry = -1;
+    uint32_t before = 0, its = 0;
+    auto find = [&](uint32_t v) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint64_t past = __ballot(upto[e] > v);
+            if (past && entry < 0) {
+                const int src = __builtin_ctzll(past);
+                entry = e * 64 + src;
+                its = (uint32_t)__builtin_amdgcn_readlane((int)mine[e], src);
+                before = (uint32_t)__builtin_amdgcn_readlane((int)upto[e], src) - its;
+            }
+        }
+    };
+    add();
+    const uint32_t size = kv_share(total, a.split);
+    if (!kv_keeps(total, a.n, a.split)) {
+        KvShare r = kv_share_of(u, size, total);
+        find(r.begin);
+        r.entry = entry;
+        r.first = before;
+        return r;
     }
-    KvUnit r{-1, -1, 0, 0, 0, 0, 0};
-    int32_t before = 0;
+    uint32_t steps[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int32_t upto = before + lanes_upto(mine[e]);
-        const uint64_t past = __ballot(upto > u);
-        if (past && r.entry < 0) {
-            const int src = __builtin_ctzll(past);
-            r.entry = e * 64 + src;
-            r.slot = __builtin_amdgcn_readlane(slot[e], src);
-            r.length = __builtin_amdgcn_readlane(length[e], src);
-            r.chunks = __builtin_amdgcn_readlane(mine[e], src);
-            r.first_unit = __builtin_amdgcn_readlane(upto, src) - r.chunks;
-            r.chunk = u - r.first_unit;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
+        steps[e] = mine[e];
+        mine[e] = (mine[e] + size - 1) / size;
     }
-    r.chunk_tokens = kv_even_chunk(kv_span(r.length, a.window), r.chunks);
-    return r;
+    add();
+    find(u);
+    if (entry < 0) return KvShare{0, 0, 1, 0, 0, -1};
+    uint32_t own = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e == entry >> 6) own = (uint32_t)__builtin_amdgcn_readlane((int)steps[e], entry & 63);
+    return kv_own_share(entry, own, its, u - before);
 }
 
-// The same from a plan (kv_plan_kernel) for larger batches: a.plan[i] is the units
-// before entry i.
-__device__ inline KvUnit kv_planned_unit(const KvAttend &a, int32_t u) {
-    const int32_t *before = a.plan;
-    KvUnit r{-1, -1, 0, 0, 0, 0, 0};
-    if (u >= before[a.n]) return r;
-    int32_t lo = 0, hi = (int32_t)a.n;  // before[lo] <= u < before[hi]
+// The same from a plan (kv_plan_kernel) for larger batches: a.plan[i] is the steps
+// before entry i, a.plan[n] all of them; where shares keep to sequences, a.plan[n + 1 + i]
+// is the shares before entry i.
+__device__ inline KvShare kv_planned_share(const KvAttend &a, uint32_t u) {
+    Scalar *before = scalar(a.plan);
+    const uint32_t total = (uint32_t)before[a.n];
+    const bool keeps = kv_keeps(total, a.n, a.split);
+    KvShare r = kv_share_of(u, kv_share(total, a.split), total);
+    Scalar *sums = keeps ? before + a.n + 1 : before;
+    const uint32_t v = keeps ? u : r.begin;
+    if (v >= (uint32_t)sums[a.n]) return r;
+    int32_t lo = 0, hi = (int32_t)a.n;  // sums[lo] <= v < sums[hi]
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
-        if (before[mid] <= u) lo = mid;
+        if ((uint32_t)sums[mid] <= v) lo = mid;
         else hi = mid;
     }
+    if (keeps)
+        return kv_own_share(lo, (uint32_t)before[lo + 1] - (uint32_t)before[lo], (uint32_t)sums[lo + 1] - (uint32_t)sums[lo],
+                            u - (uint32_t)sums[lo]);
     r.entry = lo;
-    r.slot = a.slots[lo];
-    r.length = kv_known_length(a.c, r.slot);
-    r.first_unit = before[lo];
-    r.chunks = before[lo + 1] - r.first_unit;
-    r.chunk = u - r.first_unit;
-    r.chunk_tokens = kv_even_chunk(kv_span(r.length, a.window), r.chunks);
+    r.first = (uint32_t)before[lo];
     return r;
 }
 
-// Where no entry can have two chunks, unit u is entry u.
-__device__ inline KvUnit kv_whole_unit(const KvAttend &a, int32_t u) {
-    KvUnit r{-1, -1, 0, 0, 1, u, kKvMostTokens};
-    if (u >= a.n) return r;
-    r.entry = u;
-    r.slot = a.slots[u];
-    r.length = kv_known_length(a.c, r.slot);
-    return r;
-}
+// A share's part of one entry: its tokens from `from` to `to`, of those from `begin` on.
+struct KvWork {
+    int32_t entry, slot, length, begin, from, to;
+    uint32_t steps;    // of the entry
+    bool whole, last;  // all of the entry; the share ends with it
+};
 
 __global__ void __launch_bounds__(1024) kv_plan_kernel(KvAttend a);
 
-// One workgroup: one chunk of one entry's tokens, one key head, 16 R of its query
-// heads ("rows").  Its four waves take the chunk's 32-token tiles in turn, each
-// with a running maximum and sum of its own, and are joined at the end.
+// One workgroup: an equal share of the batch's tokens, mostly a part of one entry's,
+// one key head, 16 R of its query heads ("rows").  Its waves take the 32-token tiles in
+// turn, each with a running maximum and sum of its own, and are joined at the end of
+// an entry's part.
 //
 // Scores are taken transposed, S^T = K Q^T (16 tokens x 16 rows, head_dim / 32
 // MFMAs): a lane then holds eight of the tile's tokens of one row, which are the
@@ -215,78 +242,70 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     constexpr float kSlack = 8.f;
     constexpr int SZ = E4M3 ? 1 : 2;
     const KvView &c = a.c;
-    const int lane = (int)(threadIdx.x & 63), wave = uniform((int)(threadIdx.x >> 6));
-    const int col = lane & 15, g = lane >> 4;
+    const int wave = uniform((int)(threadIdx.x >> 6));
 
     // Blocks of the same keys differ by 8, so that they share an XCD's L2.
     const int32_t rg = (int32_t)((blockIdx.x >> 3) % (unsigned)a.row_groups);
     const int32_t uh = (int32_t)((blockIdx.x >> 3) / (unsigned)a.row_groups * 8 + (blockIdx.x & 7));
     const int32_t unit = (int32_t)((uint32_t)uh / (uint32_t)c.kv_heads), head = uh - unit * c.kv_heads;
-    const KvUnit w = !a.where       ? kv_whole_unit(a, unit)
-                     : a.plan       ? kv_planned_unit(a, unit)
-                     : a.n <= 64    ? kv_find_unit<1>(a, unit)
-                     : a.n <= 128   ? kv_find_unit<2>(a, unit)
-                                    : kv_find_unit<kKvScan / 64>(a, unit);
+    KvShare w{0, 1, 1, 0, 0, unit < a.n ? unit : -1};  // without a.where a share is an entry
+    if (a.plan) w = kv_planned_share(a, (uint32_t)unit);
+    else if (a.where) w = a.n <= 64    ? kv_find_share<1>(a, (uint32_t)unit)
+                          : a.n <= 128 ? kv_find_share<2>(a, (uint32_t)unit)
+                                       : kv_find_share<kKvScan / 64>(a, (uint32_t)unit);
     if (w.entry < 0) return;
-    const int32_t entry = uniform(w.entry), chunks = uniform(w.chunks), chunk = uniform(w.chunk);
-    const int32_t slot = uniform(w.slot), length = uniform(w.length);
-    const bool known = kv_slot_ok(c, slot);
-    const int32_t begin = kv_first(length, a.window);
-    const int32_t tokens = uniform(w.chunk_tokens), from = (begin & ~(kKvTile - 1)) + chunk * tokens;
-    const int32_t to = (int32_t)min((int64_t)length, (int64_t)from + tokens);
-    if (chunk == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
-        if (a.where) {
-            a.where[2 * (int64_t)entry] = uniform(w.first_unit);
-            a.where[2 * (int64_t)entry + 1] = chunks;
-        }
-        if (!known && slot != -1) atomicAdd(c.skipped, 1ull);
-    }
+    const uint32_t share_begin = (uint32_t)uniform((int)w.begin), share_end = (uint32_t)uniform((int)w.end);
+    uint32_t first = (uint32_t)uniform((int)w.first);
+    __shared__ f32x4 so[W / 2][R * ACC / 4][64];
+    __shared__ float sm[W / 2][R][64], sl[W / 2][R][64];
 
-    const int32_t row0 = rg * 16 * R;
-    u32x4 q[R][KB];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int32_t row = row0 + 16 * r + col;
-        const bool in = row < a.group;
-        const uint16_t *src = (const uint16_t *)a.q + entry * a.q_stride + (int64_t)(head * a.group + (in ? row : 0)) * D + 8 * g;
-#pragma unroll
-        for (int j = 0; j < KB; ++j) {
-            u32x4 x;
-            if (a.q_aligned) {
-                x = *(const u32x4 *)(src + 32 * j);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = src[32 * j + 2 * e] | (uint32_t)src[32 * j + 2 * e + 1] << 16;
-            }
-            q[r][j] = in ? x : u32x4{0, 0, 0, 0};
-        }
-    }
-
-    f32x4 o[R][KB][2];  // dimensions 32 j + 2 (4 g + i) + e of row `col`: o[.][j][e][i]
-    float m[R], l[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        m[r] = -INFINITY;
-        l[r] = 0.f;
-#pragma unroll
-        for (int j = 0; j < KB; ++j) o[r][j][0] = o[r][j][1] = f32x4{0, 0, 0, 0};
-    }
-
-    // Page ids are read by scalar loads: as vector loads they would be waited for
-    // behind every key and value on its way.
-    using Scalar = const __attribute__((address_space(4))) int32_t;
-    Scalar *pages = (Scalar *)(uintptr_t)(c.table + (int64_t)(known ? slot : 0) * c.slot_pages);
-    const int32_t inside = kv_page_tokens(c) - 1;
+    const int32_t row0 = rg * 16 * R, inside = kv_page_tokens(c) - 1;
     const char *kbase = (const char *)c.k + SZ * (a.layer * c.k_layer + kv_head_base(c, head));
     const char *vbase = (const char *)c.v + SZ * (a.layer * c.v_layer + kv_head_base(c, head));
 
-    // A tile's two halves of 16 tokens lie in one page each.  The next tile's keys are
-    // asked for once this one's scores are taken, its values once this one's are used:
-    // the registers are free by then, and the rest of the tile's work hides the way.
+    // The share's part of entry i, whose first step is the batch's step `first`.
+    auto part_of = [&](int32_t i, uint32_t first) __attribute__((always_inline)) {
+        const int32_t slot = scalar(a.slots)[i];
+        const bool known = kv_slot_ok(c, slot);
+        KvWork x;
+        x.entry = i;
+        x.slot = known ? slot : 0;
+        x.length = 0;
+        if (known) {
+            const int32_t had = scalar(c.lengths)[slot], room = c.slot_pages << c.page_shift;
+            x.length = had < 0 ? 0 : min(had, room);
+        }
+        x.begin = kv_first(x.length, a.window);
+        const int32_t tile0 = x.begin & ~(kKvTile - 1);
+        x.steps = a.where ? kv_steps(x.length - tile0) : 1;
+        const KvPart part = kv_part(share_begin, share_end, first, x.steps);
+        x.whole = part.whole;
+        x.last = !a.where || first + part.to >= share_end;
+        x.from = tile0 + (int32_t)part.from * kKvStep;
+        x.to = part.to == x.steps ? x.length : tile0 + (int32_t)part.to * kKvStep;
+        if (part.from == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
+            if (a.where) {
+                a.where[2 * (int64_t)i] = unit + i;
+                a.where[2 * (int64_t)i + 1] = (int32_t)kv_parts(w.index, w.size, first, x.steps);
+            }
+            if (!known && slot != -1) atomicAdd(c.skipped, 1ull);
+        }
+        return x;
+    };
+
+    // A tile's two halves of 16 tokens lie in one page each.  Page ids are read by scalar
+    // loads: as vector loads they would be waited for behind every key and value on its
+    // way.  The next tile's keys are asked for once this one's scores are taken, its values
+    // once this one's are used, the next part's first tile and queries before this part's
+    // waves are joined: the registers are free by then, and what is left to do hides the way.
     Raw kr[2][KB], vr[2][KB];
-    auto page_of = [&](int32_t tok) { return tok < to ? pages[tok >> c.page_shift] : -1; };
-    const uint32_t kl = (uint32_t)SZ * kv_key_at(c, col, 8 * g), vl = (uint32_t)SZ * kv_value_at(c, 4 * g, 2 * col);
-    auto load_keys = [&](int32_t t, const int32_t *pg) {
+    u32x4 q[R][KB];
+    Scalar *pages = nullptr;
+    KvWork part;
+    uint32_t kl = 0, vl = 0;  // the lane's place in a tile of keys and of values
+    int32_t t = 0, here[2], next[2];
+    auto page_of = [&](int32_t tok) { return tok < part.to ? pages[tok >> c.page_shift] : -1; };
+    auto load_keys = [&](int32_t t, const int32_t *pg) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t p = kv_page_ok(c, pg[h]) ? pg[h] : 0;
@@ -295,7 +314,7 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
             for (int j = 0; j < KB; ++j) kr[h][j] = *(const Raw *)(ks + (SZ * 32 * j << c.page_shift) + kl);
         }
     };
-    auto load_values = [&](int32_t t, const int32_t *pg) {
+    auto load_values = [&](int32_t t, const int32_t *pg) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t p = kv_page_ok(c, pg[h]) ? pg[h] : 0;
@@ -304,202 +323,268 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
             for (int j = 0; j < KB; ++j) vr[h][j] = *(const Raw *)(vs + SZ * 128 * j + vl);
         }
     };
-    int32_t t = from + kKvTile * wave;
-    int32_t here[2] = {page_of(t), page_of(t + 16)};
-    int32_t next[2] = {page_of(t + kStep), page_of(t + kStep + 16)};
-    if (t < to) {
-        load_keys(t, here);
-        load_values(t, here);
-    }
-    for (; t < to; t += kStep) {
-        const bool good[2] = {kv_page_ok(c, here[0]), kv_page_ok(c, here[1])};
-        const bool more = t + kStep < to;
-        const bool full = good[0] && good[1] && t >= begin && t + kKvTile <= to;
-        u32x4 keep{~0u, ~0u, ~0u, ~0u};  // weights of tokens that count: two 16-bit ones a word
-        if (!full) {
+    // The lane is taken anew where a part begins and ends: what is computed from it would
+    // otherwise be kept in registers over the loops, some twenty of them.
+    auto fresh_lane = [] {
+        int lane = (int)(threadIdx.x & 63);
+        asm volatile("" : "+v"(lane));
+        return lane;
+    };
+    auto start = [&]() __attribute__((always_inline)) {
+        const int lane = fresh_lane(), col = lane & 15, g = lane >> 4;
+        kl = (uint32_t)SZ * kv_key_at(c, col, 8 * g);
+        vl = (uint32_t)SZ * kv_value_at(c, 4 * g, 2 * col);
+        // the queries first: what is loaded after them is not waited for with them
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int32_t tok = t + 16 * h + 4 * g + i;
-                    if (!(good[h] && tok >= begin && tok < to)) keep[2 * h + i / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
-                }
-        }
-
-        u32x4 hi[R], lo[R];
-        {
-            f32x4 s[R][2];
-#pragma unroll
-            for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < KB; ++j) {
-                    const u32x4 kk = Eight<IO, E4M3>::wide(kr[h][j]);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) s[r][h] = IO::mfma(kk, q[r][j], s[r][h]);
-                }
-            if (more) load_keys(t + kStep, next);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float x[8], top = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] = s[r][i >> 2][i & 3] * a.scale;
-                    if (!full && !((keep[i / 2] >> (16 * (i & 1))) & 1)) x[i] = -INFINITY;
-                    top = fmaxf(top, x[i]);
-                }
-                top = rows_max(top);
-                // m follows the maximum only once that is kSlack past it: until then weights
-                // up to 2^kSlack do no harm, and rescaling costs as much as a tile's scores
-                if (__ballot(!(top <= m[r] + kSlack))) {
-                    const float most = fmaxf(m[r], top), base = most == -INFINITY ? 0.f : most;
-                    const float shrink = exp2_fast(m[r] - base);
-                    m[r] = most;
-                    l[r] *= shrink;
-#pragma unroll
-                    for (int j = 0; j < KB; ++j) {
-                        o[r][j][0] *= shrink;
-                        o[r][j][1] *= shrink;
-                    }
-                }
-                const float base = m[r] == -INFINITY ? 0.f : m[r];  // nothing yet, or nothing but -infinity
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] = exp2_fast(x[i] - base);
-                    sum += x[i];
-                }
-                l[r] += sum;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    hi[r][i] = IO::pack(x[2 * i], x[2 * i + 1]);
-                    lo[r][i] = IO::pack(x[2 * i] - IO::low(hi[r][i]), x[2 * i + 1] - IO::high(hi[r][i]));
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < KB; ++j) {
-            const u32x4 v0 = Eight<IO, E4M3>::wide(vr[0][j]), v1 = Eight<IO, E4M3>::wide(vr[1][j]);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                u32x4 vv{v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1]};
-                if (!full) vv &= keep;  // 0 times what lies behind a sequence could be NaN
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    o[r][j][e] = IO::mfma(vv, hi[r], o[r][j][e]);
-                    o[r][j][e] = IO::mfma(vv, lo[r], o[r][j][e]);
-                }
-            }
-        }
-        if (more) load_values(t + kStep, next);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            here[h] = next[h];
-            next[h] = page_of(t + 2 * kStep + 16 * h);
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) l[r] = rows_sum(l[r]);
-
-    // join the waves: the upper half into the lower, and again
-    __shared__ f32x4 so[W / 2][R * ACC / 4][64];
-    __shared__ float sm[W / 2][R][64], sl[W / 2][R][64];
-#pragma unroll
-    for (int half = W / 2; half; half >>= 1) {
-        if (wave >= half && wave < 2 * half) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                sm[wave - half][r][lane] = m[r];
-                sl[wave - half][r][lane] = l[r];
-#pragma unroll
-                for (int j = 0; j < KB; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) so[wave - half][(r * KB + j) * 2 + e][lane] = o[r][j][e];
-            }
-        }
-        __syncthreads();
-        if (wave < half) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float om = sm[wave][r][lane], next = fmaxf(m[r], om);
-                const float base = next == -INFINITY ? 0.f : next;
-                const float x = exp2_fast(m[r] - base), y = exp2_fast(om - base);
-                m[r] = next;
-                l[r] = l[r] * x + sl[wave][r][lane] * y;
-#pragma unroll
-                for (int j = 0; j < KB; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        o[r][j][e] = o[r][j][e] * x + so[wave][(r * KB + j) * 2 + e][lane] * y;
-            }
-        }
-        __syncthreads();
-    }
-    if (wave) return;
-
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int32_t row = row0 + 16 * r + col;
-        if (row >= a.group) continue;
-        const int64_t at = ((int64_t)head * a.group) + row;
-        if (chunks == 1) {
-            const int64_t to_row = (int64_t)entry * a.q_heads + at;
-            if (a.lse && g == 0) a.lse[to_row] = length ? (m[r] + log2f(l[r])) * 0.6931471805599453f : -INFINITY;
-            const float unit_v = length ? c.v_scale / l[r] : 0.f;
-            uint32_t *dst = (uint32_t *)a.out + (to_row * D + 8 * g) / 2;
-#pragma unroll
-            for (int j = 0; j < KB; ++j)
-                *(u32x4 *)(dst + 16 * j) =
-                    u32x4{IO::pack(o[r][j][0][0] * unit_v, o[r][j][1][0] * unit_v),
-                          IO::pack(o[r][j][0][1] * unit_v, o[r][j][1][1] * unit_v),
-                          IO::pack(o[r][j][0][2] * unit_v, o[r][j][1][2] * unit_v),
-                          IO::pack(o[r][j][0][3] * unit_v, o[r][j][1][3] * unit_v)};
-        } else {
-            const int64_t to_row = (int64_t)unit * a.q_heads + at;
-            if (g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(m[r], l[r]);
-            float *dst = a.part_o + to_row * D + 8 * g;
+        for (int r = 0; r < R; ++r) {
+            const int32_t row = row0 + 16 * r + col;
+            const bool in = row < a.group;
+            const uint16_t *src = (const uint16_t *)a.q + part.entry * a.q_stride +
+                                  (int64_t)(head * a.group + (in ? row : 0)) * D + 8 * g;
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
-                *(f32x4 *)(dst + 32 * j) = f32x4{o[r][j][0][0], o[r][j][1][0], o[r][j][0][1], o[r][j][1][1]};
-                *(f32x4 *)(dst + 32 * j + 4) = f32x4{o[r][j][0][2], o[r][j][1][2], o[r][j][0][3], o[r][j][1][3]};
+                u32x4 x;
+                if (a.q_aligned) {
+                    x = *(const u32x4 *)(src + 32 * j);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = src[32 * j + 2 * e] | (uint32_t)src[32 * j + 2 * e + 1] << 16;
+                }
+                q[r][j] = in ? x : u32x4{0, 0, 0, 0};
             }
         }
+        pages = scalar(c.table + (int64_t)part.slot * c.slot_pages);
+        t = part.from + kKvTile * wave;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            here[h] = page_of(t + 16 * h);
+            next[h] = page_of(t + kStep + 16 * h);
+        }
+        if (t < part.to) {
+            load_keys(t, here);
+            load_values(t, here);
+        }
+    };
+
+    part = part_of(uniform(w.entry), first);
+    start();
+    for (;;) {
+        const int lane = fresh_lane(), g = lane >> 4;
+        f32x4 o[R][KB][2];  // dimensions 32 j + 2 (4 g + i) + e of row lane % 16: o[.][j][e][i]
+        float m[R], l[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int j = 0; j < KB; ++j) o[r][j][0] = o[r][j][1] = f32x4{0, 0, 0, 0};
+        }
+
+        // A wave's last tile is code of its own: loads behind a branch would have to be
+        // waited for as if they might not be there, that is all of them at each use.
+        auto tile = [&](auto another) __attribute__((always_inline)) {
+            constexpr bool more = decltype(another)::value;
+            const bool good[2] = {kv_page_ok(c, here[0]), kv_page_ok(c, here[1])};
+            const bool full = good[0] && good[1] && t >= part.begin && t + kKvTile <= part.to;
+            u32x4 keep{~0u, ~0u, ~0u, ~0u};  // weights of tokens that count: two 16-bit ones a word
+            if (!full) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t tok = t + 16 * h + 4 * g + i;
+                        if (!(good[h] && tok >= part.begin && tok < part.to)) keep[2 * h + i / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
+                    }
+            }
+
+            u32x4 hi[R], lo[R];
+            {
+                f32x4 s[R][2];
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        const u32x4 kk = Eight<IO, E4M3>::wide(kr[h][j]);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) s[r][h] = IO::mfma(kk, q[r][j], s[r][h]);
+                    }
+                if (more) load_keys(t + kStep, next);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float x[8], top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[i] = s[r][i >> 2][i & 3] * a.scale;
+                        if (!full && !((keep[i / 2] >> (16 * (i & 1))) & 1)) x[i] = -INFINITY;
+                        top = fmaxf(top, x[i]);
+                    }
+                    top = rows_max(top);
+                    // m follows the maximum only once that is kSlack past it: until then weights
+                    // up to 2^kSlack do no harm, and rescaling costs as much as a tile's scores
+                    if (__ballot(!(top <= m[r] + kSlack))) {
+                        const float most = fmaxf(m[r], top), base = most == -INFINITY ? 0.f : most;
+                        const float shrink = exp2_fast(m[r] - base);
+                        m[r] = most;
+                        l[r] *= shrink;
+#pragma unroll
+                        for (int j = 0; j < KB; ++j) {
+                            o[r][j][0] *= shrink;
+                            o[r][j][1] *= shrink;
+                        }
+                    }
+                    const float base = m[r] == -INFINITY ? 0.f : m[r];  // nothing yet, or nothing but -infinity
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[i] = exp2_fast(x[i] - base);
+                        sum += x[i];
+                    }
+                    l[r] += sum;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        hi[r][i] = IO::pack(x[2 * i], x[2 * i + 1]);
+                        lo[r][i] = IO::pack(x[2 * i] - IO::low(hi[r][i]), x[2 * i + 1] - IO::high(hi[r][i]));
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                const u32x4 v0 = Eight<IO, E4M3>::wide(vr[0][j]), v1 = Eight<IO, E4M3>::wide(vr[1][j]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    u32x4 vv{v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1]};
+                    if (!full) vv &= keep;  // 0 times what lies behind a sequence could be NaN
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        o[r][j][e] = IO::mfma(vv, hi[r], o[r][j][e]);
+                        o[r][j][e] = IO::mfma(vv, lo[r], o[r][j][e]);
+                    }
+                }
+            }
+            if (more) load_values(t + kStep, next);
+        };
+        for (; t + kStep < part.to; t += kStep) {
+            tile(std::true_type());
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                here[h] = next[h];
+                next[h] = page_of(t + 2 * kStep + 16 * h);
+            }
+        }
+        if (t < part.to) tile(std::false_type());
+#pragma unroll
+        for (int r = 0; r < R; ++r) l[r] = rows_sum(l[r]);
+
+        const KvWork done = part;
+        if (!done.last) {  // the share goes on with the next entry
+            first += part.steps;
+            part = part_of(part.entry + 1, first);
+            start();
+        }
+
+        // join the waves: the upper half into the lower, and again
+#pragma unroll
+        for (int half = W / 2; half; half >>= 1) {
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    sm[wave - half][r][lane] = m[r];
+                    sl[wave - half][r][lane] = l[r];
+#pragma unroll
+                    for (int j = 0; j < KB; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) so[wave - half][(r * KB + j) * 2 + e][lane] = o[r][j][e];
+                }
+            }
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float om = sm[wave][r][lane], next = fmaxf(m[r], om);
+                    const float base = next == -INFINITY ? 0.f : next;
+                    const float x = exp2_fast(m[r] - base), y = exp2_fast(om - base);
+                    m[r] = next;
+                    l[r] = l[r] * x + sl[wave][r][lane] * y;
+#pragma unroll
+                    for (int j = 0; j < KB; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            o[r][j][e] = o[r][j][e] * x + so[wave][(r * KB + j) * 2 + e][lane] * y;
+                }
+            }
+            __syncthreads();
+        }
+        if (wave == 0) {
+            const int lane = fresh_lane(), col = lane & 15, g = lane >> 4;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int32_t row = row0 + 16 * r + col;
+                if (row >= a.group) continue;
+                const int64_t at = ((int64_t)head * a.group) + row;
+                if (done.whole) {
+                    const int64_t to_row = (int64_t)done.entry * a.q_heads + at;
+                    if (a.lse && g == 0) a.lse[to_row] = done.length ? (m[r] + log2f(l[r])) * 0.6931471805599453f : -INFINITY;
+                    const float unit_v = done.length ? c.v_scale / l[r] : 0.f;
+                    uint32_t *dst = (uint32_t *)a.out + (to_row * D + 8 * g) / 2;
+#pragma unroll
+                    for (int j = 0; j < KB; ++j)
+                        *(u32x4 *)(dst + 16 * j) =
+                            u32x4{IO::pack(o[r][j][0][0] * unit_v, o[r][j][1][0] * unit_v),
+                                  IO::pack(o[r][j][0][1] * unit_v, o[r][j][1][1] * unit_v),
+                                  IO::pack(o[r][j][0][2] * unit_v, o[r][j][1][2] * unit_v),
+                                  IO::pack(o[r][j][0][3] * unit_v, o[r][j][1][3] * unit_v)};
+                } else {
+                    const int64_t to_row = (int64_t)(unit + done.entry) * a.q_heads + at;
+                    if (g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(m[r], l[r]);
+                    float *dst = a.part_o + to_row * D + 8 * g;
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        *(f32x4 *)(dst + 32 * j) = f32x4{o[r][j][0][0], o[r][j][1][0], o[r][j][0][1], o[r][j][1][1]};
+                        *(f32x4 *)(dst + 32 * j + 4) = f32x4{o[r][j][0][2], o[r][j][1][2], o[r][j][0][3], o[r][j][1][3]};
+                    }
+                }
+            }
+        }
+        if (done.last) return;
     }
 }
 
-// Joins the chunks of entries that have more than one.  A row's numbers are dealt to
+// Joins the parts of entries that have more than one.  A row's numbers are dealt to
 // D / 4 threads; a workgroup takes ROWS query heads of an entry with as many teams as
-// are left over, each with a part of the chunks: one row where few are to be joined
-// (they have the most chunks), eight where many are (mostly to find that there is
+// are left over, each with some of the parts: one row where few are to be joined
+// (they have the most parts), eight where many are (mostly to find that there is
 // nothing to join: 3,584 workgroups that only leave take 5 us to start).
+constexpr int kv_join_threads(int D, bool many) { return many || D < 128 ? 256 : 512; }
+
 template <typename IO, int D, bool MANY>
-__global__ void __launch_bounds__(256) kv_join_kernel(KvAttend a) {
-    constexpr int COLS = D / 4, SETS = 256 / COLS, ROWS = MANY ? SETS : 1, TEAMS = SETS / ROWS;
+__global__ void __launch_bounds__(kv_join_threads(D, MANY)) kv_join_kernel(KvAttend a) {
+    constexpr int COLS = D / 4, SETS = kv_join_threads(D, MANY) / COLS, ROWS = MANY ? SETS : 1, TEAMS = SETS / ROWS;
     const int32_t per_entry = (a.q_heads + ROWS - 1) / ROWS;
     const int64_t entry = blockIdx.x / (unsigned)per_entry;
-    const int32_t first = a.where[2 * entry], chunks = a.where[2 * entry + 1];
-    if (chunks <= 1) return;
+    const int32_t first = a.where[2 * entry], parts = a.where[2 * entry + 1];
+    if (parts <= 1) return;
     const int col = (int)threadIdx.x % COLS, set = (int)threadIdx.x / COLS, team = set / ROWS;
     const int32_t row = (int32_t)(blockIdx.x % (unsigned)per_entry) * ROWS + set % ROWS;
     const bool in = team < TEAMS && row < a.q_heads;
     __shared__ f32x4 so[TEAMS][COLS];
-    __shared__ float sml[TEAMS][2];
+    __shared__ float sm[TEAMS], sl[TEAMS];
     float m = -INFINITY, l = 0.f;
     f32x4 o{0, 0, 0, 0};
     if (in) {
-        constexpr int UP = 4;  // chunks whose numbers are on their way at once
-        for (int32_t k0 = team; k0 < chunks; k0 += UP * TEAMS) {
+        constexpr int UP = MANY ? 4 : 8;  // parts whose numbers are on their way at once
+        for (int32_t k0 = team; k0 < parts; k0 += UP * TEAMS) {
             float2 ml[UP];
             f32x4 po[UP];
             float most = m;
 #pragma unroll
             for (int i = 0; i < UP; ++i) {
                 const int32_t k = k0 + i * TEAMS;
-                const int64_t at = (int64_t)(first + (k < chunks ? k : k0)) * a.q_heads + row;
+                const int64_t at = (int64_t)(first + (k < parts ? k : k0)) * a.q_heads + row;
                 ml[i] = *(const float2 *)(a.part_ml + 2 * at);
                 po[i] = *(const f32x4 *)(a.part_o + at * D + 4 * col);
-                if (k >= chunks) ml[i] = make_float2(-INFINITY, 0.f);
+                if (k >= parts) ml[i] = make_float2(-INFINITY, 0.f);
             }
 #pragma unroll
             for (int i = 0; i < UP; ++i) most = fmaxf(most, ml[i].x);
@@ -509,7 +594,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(KvAttend a) {
             o *= x;
 #pragma unroll
             for (int i = 0; i < UP; ++i) {
-                if (k0 + i * TEAMS >= chunks) break;
+                if (k0 + i * TEAMS >= parts) break;
                 const float y = exp2_fast(ml[i].x - base);
                 l += ml[i].y * y;
                 o += po[i] * y;
@@ -517,22 +602,25 @@ __global__ void __launch_bounds__(256) kv_join_kernel(KvAttend a) {
         }
     }
     if (TEAMS > 1) {
+        if (in && col == 0) sm[team] = m;
+        __syncthreads();
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < TEAMS; ++k) most = fmaxf(most, sm[k]);
+        const float x = exp2_fast(m - (most == -INFINITY ? 0.f : most));
+        m = most;
+        l *= x;
+        o *= x;
         if (in) {
             so[team][col] = o;
-            if (col == 0) {
-                sml[team][0] = m;
-                sml[team][1] = l;
-            }
+            if (col == 0) sl[team] = l;
         }
         __syncthreads();
         if (team) return;
 #pragma unroll
         for (int k = 1; k < TEAMS; ++k) {
-            const float om = sml[k][0], most = fmaxf(m, om), base = most == -INFINITY ? 0.f : most;
-            const float x = exp2_fast(m - base), y = exp2_fast(om - base);
-            m = most;
-            l = l * x + sml[k][1] * y;
-            o = o * x + so[k][col] * y;
+            l += sl[k];
+            o += so[k][col];
         }
     }
     if (!in) return;

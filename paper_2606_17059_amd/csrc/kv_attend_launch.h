@@ -20,11 +20,11 @@ hipError_t kv_launch_dim(const KvAttend &a, hipStream_t st) {
         kv_attend_kernel<IO, E4M3, D, 2, kKvWaves><<<grid, block, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.where) return e;
-    constexpr int kSets = 256 / (D / 4);
+    constexpr int kSets = kv_join_threads(D, true) / (D / 4);
     if (a.n * a.q_heads > kKvJoinMany)
-        kv_join_kernel<IO, D, true><<<dim3((unsigned)(a.n * ((a.q_heads + kSets - 1) / kSets))), dim3(256), 0, st>>>(a);
+        kv_join_kernel<IO, D, true><<<dim3((unsigned)(a.n * ((a.q_heads + kSets - 1) / kSets))), dim3(kv_join_threads(D, true)), 0, st>>>(a);
     else
-        kv_join_kernel<IO, D, false><<<dim3((unsigned)(a.n * a.q_heads)), dim3(256), 0, st>>>(a);
+        kv_join_kernel<IO, D, false><<<dim3((unsigned)(a.n * a.q_heads)), dim3(kv_join_threads(D, false)), 0, st>>>(a);
     return hipGetLastError();
 }
 

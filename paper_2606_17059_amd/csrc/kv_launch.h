@@ -20,13 +20,13 @@ struct KvAttend {
     int64_t q_stride;
     void *out;
     float *lse;
-    int32_t *where;  // per entry: its first unit and its chunks (nullptr: no entry has two)
-    int32_t *plan;   // see kv_planned_unit (nullptr: units are found from the lengths)
+    int32_t *where;  // per entry: its first part and their number (nullptr: no entry has two)
+    int32_t *plan;   // see kv_planned_share (nullptr: shares are found from the lengths)
     float *part_o, *part_ml;
     int64_t layer;
     int32_t q_heads, group, row_groups, window;
     KvSplit split;          // of one key head's tokens
-    int32_t units;          // chunks there may be at most
+    int32_t units;          // shares there may be at most
     float scale;            // with the keys' scale and log2 e
     bool q_aligned;
     bool wide;  // one workgroup of many waves takes a sequence
@@ -43,9 +43,9 @@ constexpr int kv_rows(int group, int head_dim) { return group > 16 && head_dim <
 // spill (64 sequences of 2,000 tokens, 4 key heads: 112 us with one, 124 with two).
 constexpr int kv_resident(bool e4m3, int head_dim, int rows, int waves) {
     const int n = head_dim * rows;
-    const int chunked = e4m3 ? (n <= 64 ? 6 : (n <= 128 ? 4 : (n <= 192 ? 3 : 2)))
-                             : (n <= 64 ? 5 : (n <= 96 ? 4 : (n <= 128 ? 3 : (head_dim < 256 ? 2 : 1))));
-    return waves == kKvWaves ? chunked : waves / 4;
+    const int many = e4m3 ? (n <= 64 ? 5 : (n <= 128 ? 4 : (n <= 192 ? 3 : 2)))
+                          : (n <= 64 ? 5 : (n <= 96 ? 4 : (n <= 128 ? 3 : (head_dim < 256 ? 2 : 1))));
+    return waves == kKvWaves ? many : waves / 4;
 }
 
 // Waves of a workgroup that takes a whole short sequence.

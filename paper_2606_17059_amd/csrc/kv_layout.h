@@ -53,7 +53,7 @@ PR_KV_FN int64_t kv_head_base(const KvView &c, int32_t head) {
 // ---- how attention splits a batch ---------------------------------------------
 constexpr int32_t kKvMostTokens = 1 << 30;  // of a sequence
 constexpr int kKvTile = 32;        // tokens a wave takes at a time
-constexpr int kKvWaves = 4;        // waves of a workgroup that takes a chunk
+constexpr int kKvWaves = 4;        // waves of a workgroup that takes a share of a batch
 constexpr int kKvStep = kKvTile * kKvWaves;
 
 // First token attended, rounded down to a tile, and the tiles' tokens from there.
@@ -64,44 +64,47 @@ PR_KV_FN int32_t kv_span(int32_t length, int32_t window) {
     return length - (kv_first(length, window) & ~(kKvTile - 1));
 }
 
-// A span in blocks: 256 sequences' blocks can be added in 32 bits.
-constexpr int kKvBlock = 256;
-PR_KV_FN int32_t kv_blocks(int32_t span) { return (span + kKvBlock - 1) / kKvBlock; }
+// Steps of a workgroup that a span takes (one where there is nothing: its output is
+// written too).
+PR_KV_FN uint32_t kv_steps(int32_t span) {
+    return span <= 0 ? 1 : ((uint32_t)span + kKvStep - 1) / kKvStep;
+}
 
-// How a batch's tokens are cut: `fill` chunks occupy the GPU once; chunks longer
-// than `worth` are cut further, into `most` of them, for the sake of an even end;
-// no chunk is shorter than `least`.
+// How a batch's steps, one sequence's after another's, are cut into equal shares: `fill`
+// of them occupy the GPU once, and none is shorter than `least`.
 struct KvSplit {
-    int32_t fill, most, least, worth;
+    uint32_t fill, least;
 };
-
-// Tokens a chunk has at most, in whole steps of a workgroup.
-PR_KV_FN int32_t kv_chunk_tokens(int32_t blocks, const KvSplit &s) {
-    const uint32_t steps = (uint32_t)blocks * (kKvBlock / kKvStep), worth = (uint32_t)(s.worth / kKvStep);
-    uint32_t c = (steps + (uint32_t)s.fill - 1) / (uint32_t)s.fill;
-    if (c > worth) {
-        const uint32_t cut = (steps + (uint32_t)s.most - 1) / (uint32_t)s.most;
-        c = cut > worth ? cut : worth;
-    }
-    if (c >= (uint32_t)kKvMostTokens / kKvStep) return kKvMostTokens;
-    return (int32_t)(c * kKvStep) < s.least ? s.least : (int32_t)(c * kKvStep);
-}
-// The chunk that makes about `fill` units of what `units` of length c were.
-PR_KV_FN int32_t kv_longer_chunk(int32_t c, int32_t units, int32_t fill) {
-    const uint64_t x = (uint64_t)((uint32_t)c / kKvStep) * (uint32_t)units / (uint32_t)fill + 1;
-    return x >= (uint64_t)kKvMostTokens / kKvStep ? kKvMostTokens : (int32_t)(x * kKvStep);
+PR_KV_FN uint32_t kv_share(uint32_t steps, const KvSplit &s) {
+    const uint32_t c = (steps + s.fill - 1) / s.fill;
+    return c < s.least ? s.least : c;
 }
 
-// Chunks of one sequence (one where it has no tokens: its output is written too).
-PR_KV_FN int32_t kv_chunks(int32_t span, int32_t chunk) {
-    return span <= chunk ? 1 : (int32_t)(((uint32_t)span + (uint32_t)chunk - 1) / (uint32_t)chunk);
-}
+// Whether shares keep to sequences instead: one for each, or equal ones of a sequence
+// longer than a share.  So it is where there are more sequences than shares and they
+// are short: a share of several would begin anew with each, where workgroups beside it
+// could (600 sequences of 10 to 600 tokens on 4 key heads of 128: 82 us, 87 across;
+// 128 of 4,096 to 16,384 on 8: 935 us, 910 across).
+constexpr uint32_t kKvShort = 8;   // steps of a short sequence, on average
+PR_KV_FN bool kv_keeps(uint32_t steps, int64_t n, const KvSplit &s) { return n >= s.fill && steps < n * kKvShort; }
+PR_KV_FN uint32_t kv_even(uint32_t steps, uint32_t shares) { return (steps + shares - 1) / shares; }
 
-// A sequence's chunks made even.
-PR_KV_FN int32_t kv_even_chunk(int32_t span, int32_t chunks) {
-    if (chunks <= 1) return kKvMostTokens;
-    const uint32_t steps = ((uint32_t)span + kKvStep - 1) / kKvStep;
-    return (int32_t)((steps + (uint32_t)chunks - 1) / (uint32_t)chunks * kKvStep);
+// A share's part [from, to) of a sequence that has the steps [first, first + steps) of
+// the batch, in steps of the sequence.
+struct KvPart {
+    uint32_t from, to;
+    bool whole;  // the sequence has no other part
+};
+PR_KV_FN KvPart kv_part(uint32_t begin, uint32_t end, uint32_t first, uint32_t steps) {
+    KvPart p;
+    p.from = begin > first ? begin - first : 0;
+    p.to = end < first + steps ? end - first : steps;
+    p.whole = p.from == 0 && p.to == steps;
+    return p;
+}
+// Parts of a sequence, the first of which is in share `share`.
+PR_KV_FN uint32_t kv_parts(uint32_t share, uint32_t c, uint32_t first, uint32_t steps) {
+    return (first + steps - 1) / c - share + 1;
 }
 
 }  // namespace pr

@@ -684,27 +684,30 @@ __global__ void __launch_bounds__(256) kv_compact_move_kernel(KvCompact x, int32
     }
 }
 
-// ---- attention's split of large batches --------------------------------------------------
+// ---- attention's split of large batches, see kv_planned_share --------------------------------
 __global__ void __launch_bounds__(kKvPlanThreads) kv_plan_kernel(KvAttend a) {
     const int tid = (int)threadIdx.x;
-    uint32_t mine = 0, total = 0;  // blocks
-    auto span = [&](int64_t i) {
+    auto steps = [&](int64_t i) -> uint32_t {
+        if (i >= a.n) return 0;
         const int32_t s = a.slots[i];
-        return kv_span(kv_slot_ok(a.c, s) ? kv_length(a.c, s) : 0, a.window);
+        return kv_steps(kv_span(kv_slot_ok(a.c, s) ? kv_length(a.c, s) : 0, a.window));
     };
-    for (int64_t i = tid; i < a.n; i += kKvPlanThreads) mine = kv_add(mine, (uint32_t)kv_blocks(span(i)));
-    kv_block_before(mine, &total);
-    const uint32_t most = INT32_MAX / (kKvBlock / kKvStep);
-    const int32_t chunk = kv_chunk_tokens((int32_t)min(total, most), a.split);
-    uint32_t before = 0;
-    for (int64_t i0 = 0; i0 < a.n; i0 += kKvPlanThreads) {
-        const int64_t i = i0 + tid;
-        uint32_t all = 0;
-        const uint32_t at = before + kv_block_before(i < a.n ? (uint32_t)kv_chunks(span(i), chunk) : 0, &all);
-        if (i < a.n) a.plan[i] = (int32_t)at;
-        before += all;
-    }
-    if (tid == 0) a.plan[a.n] = (int32_t)before;
+    auto sums = [&](int32_t *out, auto of) {
+        uint32_t before = 0;
+        for (int64_t i0 = 0; i0 < a.n; i0 += kKvPlanThreads) {
+            const int64_t i = i0 + tid;
+            uint32_t all = 0;
+            const uint32_t at = before + kv_block_before(of(i), &all);
+            if (i < a.n) out[i] = (int32_t)at;
+            before += all;
+        }
+        if (tid == 0) out[a.n] = (int32_t)before;
+        return before;
+    };
+    const uint32_t total = sums(a.plan, steps);
+    if (!kv_keeps(total, a.n, a.split)) return;
+    const uint32_t size = kv_share(total, a.split);
+    sums(a.plan + a.n + 1, [&](int64_t i) { return (steps(i) + size - 1) / size; });
 }
 
 }  // namespace pr

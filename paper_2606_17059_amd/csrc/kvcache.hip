@@ -44,6 +44,7 @@ class DeviceScope {
 
 constexpr int64_t kMostGrid = ((int64_t)1 << 32) / 256 - 1;  // workgroups of 256 threads in a launch
 constexpr int64_t kMostEntries = ((int64_t)1 << 32) / pr::kKvPageThreads - 2;  // of a fork or trim, a workgroup each
+constexpr int64_t kMostSpan = (int64_t)pr::kKvStep << 31;  // tokens of a batch's tables: their steps are counted in 32 bits
 constexpr int64_t kMostRows = INT32_MAX;
 
 int element_bytes(const pr_kv *c) { return c->dtype == PR_KV_E4M3 ? 1 : 2; }
@@ -158,13 +159,7 @@ int64_t compact_parts(const pr_kv *c, void *work, pr::KvCompact *x) {
     return p.bytes;
 }
 
-#ifndef PR_KV_ROUNDS
-#define PR_KV_ROUNDS 4
-#endif
-#ifndef PR_KV_WORTH
-#define PR_KV_WORTH 1024
-#endif
-constexpr int kComputeUnits = 256, kRounds = PR_KV_ROUNDS, kWorth = PR_KV_WORTH;
+constexpr int kComputeUnits = 256;
 
 // The parts of an attention's split that go by the host's numbers (a.window and
 // the cache's sizes among them), and its workspace.
@@ -186,21 +181,23 @@ int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window,
     a->row_groups = (group + 16 * rows - 1) / (16 * rows);
     const int32_t heads = c->kv_heads * a->row_groups;
     const int32_t beside = kComputeUnits * pr::kv_resident(e4m3, c->head_dim, rows, pr::kKvWaves);
-    a->split.fill = std::max(1, beside / heads);
-    a->split.most = std::max(1, kRounds * beside / heads);
-    a->split.least = n * heads * 8 >= beside ? 512 : 256;
-    a->split.worth = kWorth;
-    const int64_t each = a->wide ? 1 : (span + a->split.least - 1) / a->split.least;
-    const int64_t units = std::min<int64_t>(n * each, a->split.most + n);
+    a->split.fill = (uint32_t)std::max(1, beside / heads);
+    a->split.least = n * heads * 8 >= beside ? 4 : 2;
+    const int64_t steps = (span + pr::kKvStep - 1) / pr::kKvStep;  // of a sequence, at most
+    const bool split = !a->wide && steps > a->split.least;
+    // shares across sequences are at most `fill`, shares that keep to them one more for each
+    const int64_t most = a->split.fill + (n >= a->split.fill ? n : 0);
+    const int64_t units = split ? std::min<int64_t>(n * steps, most) : n;
     a->units = (int32_t)std::min<int64_t>(units, INT32_MAX);
     a->where = a->plan = nullptr;
     a->part_ml = a->part_o = nullptr;
-    if (each <= 1) return 0;
+    if (!split) return 0;
     Parts p(work);
+    const int64_t parts = units + n;  // a share that goes on to the next sequence has two
     a->where = p.take<int32_t>(2 * n);
-    a->plan = n > pr::kKvScan ? p.take<int32_t>(n + 1) : nullptr;
-    a->part_ml = p.take<float>(units * q_heads * 2);
-    a->part_o = p.take<float>(units * q_heads * c->head_dim);
+    a->plan = n > pr::kKvScan ? p.take<int32_t>(2 * n + 2) : nullptr;
+    a->part_ml = p.take<float>(parts * q_heads * 2);
+    a->part_o = p.take<float>(parts * q_heads * c->head_dim);
     return p.bytes;
 }
 
@@ -242,6 +239,7 @@ pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, in
     } else if (call == PR_KV_WORK_ATTEND) {
         if (m < 1 || m % c->kv_heads) return fail(PR_EINVAL, "q_heads must be a positive multiple of kv_heads");
         if (n * m > kMostGrid) return fail(PR_EINVAL, "the batch has too many entries and query heads");
+        if (n * c->slot_pages * c->page_tokens >= kMostSpan) return fail(PR_EINVAL, "the batch may have too many tokens");
         pr::KvAttend a;
         *bytes = attend_parts(c, n, (int32_t)m, 0, nullptr, &a);
     } else if (call == PR_KV_WORK_CHANGE) {
@@ -322,6 +320,7 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
     if (!std::isfinite(scale)) return fail(PR_EINVAL, "scale must be finite");
     if (n < 0) return fail(PR_EINVAL, "n is negative");
     if (n > kMostGrid / q_heads) return fail(PR_EINVAL, "the batch has too many entries and query heads");
+    if (n * c->slot_pages * c->page_tokens >= kMostSpan) return fail(PR_EINVAL, "the batch may have too many tokens");
     if (n == 0) return ok();
     if (!slots || !q || !out) return fail(PR_EINVAL, "NULL device pointer");
     if ((uintptr_t)q & 1) return fail(PR_EINVAL, "q must be 2-byte aligned");

@@ -40,18 +40,18 @@ static void one(std::mt19937 &rng) {
     const int n = kv_length(c, 0), window = pick(0, 2) ? 0 : pick(1, room + 9);
     CHECK(n >= 0 && n <= room);
     const int begin = kv_first(n, window), span = kv_span(n, window);
-    KvSplit s{pick(1, 64), 0, pick(1, 2) * 256, pick(1, 8) * 256};
-    s.most = s.fill * pick(1, 4);
-    const int chunks = kv_chunks(span, kv_chunk_tokens((pick(0, 1) ? 1 : 64) * kv_blocks(span), s));
-    const int chunk = kv_even_chunk(span, chunks), head = pick(0, c.kv_heads - 1);
-    CHECK(chunk % kKvStep == 0);
+    const int head = pick(0, c.kv_heads - 1), waves = pick(0, 1) ? kKvWaves : 4 * kKvWaves;
+    // the sequence somewhere in a batch, cut into shares
+    const uint32_t steps = kv_steps(span), first = (uint32_t)pick(0, 50), size = (uint32_t)pick(1, 40);
     std::vector<int> keys((size_t)n * D), values((size_t)n * D), counted(n);
     const int part = D * T;  // elements of a head in a page
-    for (int k = 0; k < chunks; ++k) {
-        const int from = (begin & ~(kKvTile - 1)) + k * chunk;
-        const int to = (int)std::min<int64_t>(n, (int64_t)from + chunk);
-        for (int wave = 0; wave < kKvWaves; ++wave)
-            for (int t = from + kKvTile * wave; t < to; t += kKvStep)
+    for (uint32_t u = first / size; u * size < first + steps; ++u) {
+        const KvPart kp = kv_part(u * size, (u + 1) * size, first, steps);
+        const int from = (begin & ~(kKvTile - 1)) + (int)kp.from * kKvStep;
+        const int to = kp.to == steps ? n : (begin & ~(kKvTile - 1)) + (int)kp.to * kKvStep;
+        CHECK(kp.from < kp.to && kp.to <= steps && to <= n);
+        for (int wave = 0; wave < waves; ++wave)
+            for (int t = from + kKvTile * wave; t < to; t += kKvTile * waves)
                 for (int h = 0; h < 2; ++h) {
                     const int tok = t + 16 * h;
                     if (tok < to) CHECK((tok >> c.page_shift) < c.slot_pages);  // the table entry that is read
@@ -97,35 +97,73 @@ static void one(std::mt19937 &rng) {
         }
 }
 
-// The split never makes more chunks than a launch has room for.
+// The shares of a batch cover every sequence's steps once, are no more than a launch
+// has, and number the parts of a sequence in a row that no other has.
 static void split(std::mt19937 &rng) {
     auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); };
     const int n = pick(1, 60);
-    KvSplit s{pick(1, 200), 0, 256, pick(1, 8) * 256};
-    s.most = s.fill * pick(1, 4);
+    const KvSplit s{(uint32_t)pick(1, 200), (uint32_t)pick(1, 2) * 2};
+    const bool shorts = pick(0, 1);
     std::vector<int> spans(n);
-    int64_t units = 0;
-    int32_t total = 0;
-    for (auto &x : spans) total += kv_blocks(x = pick(0, 5) ? pick(0, 400) : pick(0, 200000));
-    int chunk = kv_chunk_tokens(total, s);
-    for (int tries = n < s.fill ? pick(0, 3) : 0; tries; --tries) {
-        int64_t now = 0;
-        for (int x : spans) now += kv_chunks(x, chunk);
-        const int longer = kv_longer_chunk(chunk, (int)now, s.fill);
-        CHECK(longer % kKvStep == 0 && longer >= kKvStep);
-        if (now > s.fill) {
-            CHECK(longer > chunk);
-            chunk = longer;
+    std::vector<uint32_t> first(n + 1, 0);
+    uint32_t longest = 0;
+    for (int i = 0; i < n; ++i) {
+        spans[i] = shorts || pick(0, 5) ? pick(0, 400) : pick(0, 200000);
+        first[i + 1] = first[i] + kv_steps(spans[i]);
+        longest = std::max(longest, kv_steps(spans[i]));
+    }
+    const uint32_t c = kv_share(first[n], s);
+    // what the host launches
+    const int64_t units = std::min<int64_t>((int64_t)n * longest, s.fill + (n >= (int)s.fill ? n : 0));
+    CHECK(c >= s.least);
+    std::vector<uint32_t> covered(n), where(n), parts(n), seen(n);
+    std::vector<int> used(units + n);
+    if (kv_keeps(first[n], n, s)) {  // shares of each sequence's own
+        int64_t u = 0;
+        for (int i = 0; i < n; ++i) {
+            const uint32_t steps = first[i + 1] - first[i], shares = (steps + c - 1) / c, even = kv_even(steps, shares);
+            for (uint32_t k = 0; k < shares; ++k, ++u) {
+                const uint32_t begin = k * even, end = std::min(begin + even, steps);
+                CHECK(u < units && even <= c);
+                if (begin >= end) continue;  // nothing is left: see the kernel's parts
+                const KvPart p = kv_part(begin, end, 0, steps);
+                CHECK(p.from == covered[i] && p.to <= steps && p.whole == (shares == 1));
+                covered[i] = p.to;
+                if (p.from == 0) {
+                    where[i] = (uint32_t)u + i;
+                    parts[i] = kv_parts(0, even, 0, steps);
+                }
+                CHECK((uint32_t)u + i == where[i] + seen[i]);
+                seen[i]++;
+                used[u + i]++;
+            }
+        }
+    } else {
+        for (int64_t u = 0; u < units; ++u) {
+            const uint32_t begin = (uint32_t)u * c, end = std::min(begin + c, first[n]);
+            if (begin >= first[n]) continue;
+            int i = 0;
+            while (first[i + 1] <= begin) ++i;
+            for (;; ++i) {
+                CHECK(i < n);
+                const uint32_t steps = first[i + 1] - first[i];
+                const KvPart p = kv_part(begin, end, first[i], steps);
+                CHECK(p.from == covered[i] && p.from < p.to && p.to <= steps && p.whole == (p.to - p.from == steps));
+                covered[i] = p.to;
+                if (p.from == 0) {
+                    where[i] = (uint32_t)u + i;
+                    parts[i] = kv_parts((uint32_t)u, c, first[i], steps);
+                    CHECK((parts[i] == 1) == p.whole);
+                }
+                CHECK((uint32_t)u + i == where[i] + seen[i] && u + i < units + n);
+                seen[i]++;
+                used[u + i]++;
+                if (first[i] + p.to >= end) break;
+            }
         }
     }
-    for (int x : spans) {
-        const int k = kv_chunks(x, chunk), even = kv_even_chunk(x, k);
-        CHECK(k == (x <= chunk ? 1 : (x + chunk - 1) / chunk));
-        CHECK((int64_t)k * even >= x && (k == 1 || even <= chunk));
-        CHECK(k <= std::max(1, (x + 255) / 256));
-        units += k;
-    }
-    CHECK(units <= (int64_t)s.most + n);
+    for (int i = 0; i < n; ++i) CHECK(covered[i] == first[i + 1] - first[i] && seen[i] == parts[i]);
+    for (int x : used) CHECK(x <= 1);
 }
 
 int main() {
