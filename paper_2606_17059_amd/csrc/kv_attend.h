@@ -237,7 +237,6 @@ template <typename IO, bool E4M3, int D, int R, int W>
 __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_kernel(KvAttend a) {
     using Raw = typename Eight<IO, E4M3>::Raw;
     constexpr int KB = D / 32;  // MFMAs of a score; pairs of 16 dimensions
-    constexpr int ACC = D / 4;  // output numbers a lane holds for a row
     constexpr int kStep = kKvTile * W;
     constexpr float kSlack = 8.f;
     constexpr int SZ = E4M3 ? 1 : 2;
@@ -256,10 +255,10 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     if (w.entry < 0) return;
     const uint32_t share_begin = (uint32_t)uniform((int)w.begin), share_end = (uint32_t)uniform((int)w.end);
     uint32_t first = (uint32_t)uniform((int)w.first);
-    __shared__ f32x4 so[W / 2][R * ACC / 4][64];
-    __shared__ float sm[W / 2][R][64], sl[W / 2][R][64];
+    __shared__ f32x4 so[W][R * KB * 2][64];
+    __shared__ float sm[W][R][16], sl[W][R][16];
 
-    const int32_t row0 = rg * 16 * R, inside = kv_page_tokens(c) - 1;
+    const int32_t row0 = rg * 16 * R, inside = kv_page_tokens(c) - 1, room = c.slot_pages << c.page_shift;
     const char *kbase = (const char *)c.k + SZ * (a.layer * c.k_layer + kv_head_base(c, head));
     const char *vbase = (const char *)c.v + SZ * (a.layer * c.v_layer + kv_head_base(c, head));
 
@@ -272,10 +271,11 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
         x.slot = known ? slot : 0;
         x.length = 0;
         if (known) {
-            const int32_t had = scalar(c.lengths)[slot], room = c.slot_pages << c.page_shift;
+            const int32_t had = scalar(c.lengths)[slot];
             x.length = had < 0 ? 0 : min(had, room);
         }
-        x.begin = kv_first(x.length, a.window);
+        x.begin = 0;
+        if (a.window > 0) x.begin = kv_first(x.length, a.window);
         const int32_t tile0 = x.begin & ~(kKvTile - 1);
         x.steps = a.where ? kv_steps(x.length - tile0) : 1;
         const KvPart part = kv_part(share_begin, share_end, first, x.steps);
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     KvWork part;
     uint32_t kl = 0, vl = 0;  // the lane's place in a tile of keys and of values
     int32_t t = 0, here[2], next[2];
-    auto page_of = [&](int32_t tok) { return tok < part.to ? pages[tok >> c.page_shift] : -1; };
+    auto page_of = [&](int32_t tok) { return tok < room ? pages[tok >> c.page_shift] : -1; };
     auto load_keys = [&](int32_t t, const int32_t *pg) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -484,70 +484,66 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
             start();
         }
 
-        // join the waves: the upper half into the lower, and again
-#pragma unroll
-        for (int half = W / 2; half; half >>= 1) {
-            if (wave >= half && wave < 2 * half) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    sm[wave - half][r][lane] = m[r];
-                    sl[wave - half][r][lane] = l[r];
-#pragma unroll
-                    for (int j = 0; j < KB; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) so[wave - half][(r * KB + j) * 2 + e][lane] = o[r][j][e];
-                }
-            }
-            __syncthreads();
-            if (wave < half) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float om = sm[wave][r][lane], next = fmaxf(m[r], om);
-                    const float base = next == -INFINITY ? 0.f : next;
-                    const float x = exp2_fast(m[r] - base), y = exp2_fast(om - base);
-                    m[r] = next;
-                    l[r] = l[r] * x + sl[wave][r][lane] * y;
-#pragma unroll
-                    for (int j = 0; j < KB; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            o[r][j][e] = o[r][j][e] * x + so[wave][(r * KB + j) * 2 + e][lane] * y;
-                }
-            }
-            __syncthreads();
-        }
-        if (wave == 0) {
-            const int lane = fresh_lane(), col = lane & 15, g = lane >> 4;
+        // Join the waves: all outputs on the largest maximum, then a wave sums the W of a
+        // pair of 16 dimensions (each lane's eight are a row's, in a row).  Two barriers;
+        // a tree takes two a level and leaves the last sums to one wave.
+        if (g == 0)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
+                sm[wave][r][lane] = m[r];
+                sl[wave][r][lane] = l[r];
+            }
+        __syncthreads();
+        float total[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float most = -INFINITY;
+            total[r] = 0.f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) most = fmaxf(most, sm[k][r][lane & 15]);
+            const float base = most == -INFINITY ? 0.f : most, x = exp2_fast(m[r] - base);
+#pragma unroll
+            for (int k = 0; k < W; ++k) total[r] += sl[k][r][lane & 15] * exp2_fast(sm[k][r][lane & 15] - base);
+            m[r] = most;
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) so[wave][(r * KB + j) * 2 + e][lane] = o[r][j][e] * x;
+        }
+        __syncthreads();
+        {
+            const int lane = fresh_lane(), col = lane & 15, g = lane >> 4;
+            for (int y = wave; y < R * KB; y += W) {
+                const int r = R == 1 ? 0 : y / KB, j = R == 1 ? y : y % KB;
                 const int32_t row = row0 + 16 * r + col;
+                f32x4 u = so[0][2 * y][lane], v = so[0][2 * y + 1][lane];
+#pragma unroll
+                for (int k = 1; k < W; ++k) {
+                    u += so[k][2 * y][lane];
+                    v += so[k][2 * y + 1][lane];
+                }
                 if (row >= a.group) continue;
+                const float most = R == 1 || r == 0 ? m[0] : m[R - 1], sum = R == 1 || r == 0 ? total[0] : total[R - 1];
                 const int64_t at = ((int64_t)head * a.group) + row;
                 if (done.whole) {
                     const int64_t to_row = (int64_t)done.entry * a.q_heads + at;
-                    if (a.lse && g == 0) a.lse[to_row] = done.length ? (m[r] + log2f(l[r])) * 0.6931471805599453f : -INFINITY;
-                    const float unit_v = done.length ? c.v_scale / l[r] : 0.f;
-                    uint32_t *dst = (uint32_t *)a.out + (to_row * D + 8 * g) / 2;
-#pragma unroll
-                    for (int j = 0; j < KB; ++j)
-                        *(u32x4 *)(dst + 16 * j) =
-                            u32x4{IO::pack(o[r][j][0][0] * unit_v, o[r][j][1][0] * unit_v),
-                                  IO::pack(o[r][j][0][1] * unit_v, o[r][j][1][1] * unit_v),
-                                  IO::pack(o[r][j][0][2] * unit_v, o[r][j][1][2] * unit_v),
-                                  IO::pack(o[r][j][0][3] * unit_v, o[r][j][1][3] * unit_v)};
+                    if (a.lse && j == 0 && g == 0)
+                        a.lse[to_row] = done.length ? (most + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                    const float unit_v = done.length ? c.v_scale / sum : 0.f;
+                    *(u32x4 *)((uint32_t *)a.out + (to_row * D + 32 * j + 8 * g) / 2) =
+                        u32x4{IO::pack(u[0] * unit_v, v[0] * unit_v), IO::pack(u[1] * unit_v, v[1] * unit_v),
+                              IO::pack(u[2] * unit_v, v[2] * unit_v), IO::pack(u[3] * unit_v, v[3] * unit_v)};
                 } else {
                     const int64_t to_row = (int64_t)(unit + done.entry) * a.q_heads + at;
-                    if (g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(m[r], l[r]);
-                    float *dst = a.part_o + to_row * D + 8 * g;
-#pragma unroll
-                    for (int j = 0; j < KB; ++j) {
-                        *(f32x4 *)(dst + 32 * j) = f32x4{o[r][j][0][0], o[r][j][1][0], o[r][j][0][1], o[r][j][1][1]};
-                        *(f32x4 *)(dst + 32 * j + 4) = f32x4{o[r][j][0][2], o[r][j][1][2], o[r][j][0][3], o[r][j][1][3]};
-                    }
+                    if (j == 0 && g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(most, sum);
+                    float *dst = a.part_o + to_row * D + 32 * j + 8 * g;
+                    *(f32x4 *)dst = f32x4{u[0], v[0], u[1], v[1]};
+                    *(f32x4 *)(dst + 4) = f32x4{u[2], v[2], u[3], v[3]};
                 }
             }
         }
         if (done.last) return;
+        __syncthreads();  // the arrays are the next part's from here
     }
 }
 

@@ -13,7 +13,7 @@ hipError_t kv_launch_dim(const KvAttend &a, hipStream_t st) {
     const dim3 grid((unsigned)(pairs * a.row_groups)), block(64 * kKvWaves);
     const int rows = kv_rows(a.group, D);
     if (a.wide)
-        kv_attend_kernel<IO, E4M3, D, 1, kv_wide(D)><<<grid, dim3(64 * kv_wide(D)), 0, st>>>(a);
+        kv_attend_kernel<IO, E4M3, D, 1, kKvWideWaves><<<grid, dim3(64 * kKvWideWaves), 0, st>>>(a);
     else if (rows == 1)
         kv_attend_kernel<IO, E4M3, D, 1, kKvWaves><<<grid, block, 0, st>>>(a);
     else if constexpr (kv_rows(17, D) == 2)

@@ -48,8 +48,7 @@ constexpr int kv_resident(bool e4m3, int head_dim, int rows, int waves) {
     return waves == kKvWaves ? many : waves / 4;
 }
 
-// Waves of a workgroup that takes a whole short sequence.
-constexpr int kv_wide(int head_dim) { return head_dim <= 96 ? 16 : 8; }
+constexpr int kKvWideWaves = 8;  // waves of a workgroup that takes a whole short sequence
 
 constexpr int kKvJoinMany = 1024;  // rows from which a joining workgroup takes several
 

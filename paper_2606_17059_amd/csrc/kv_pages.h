@@ -403,10 +403,11 @@ __device__ __forceinline__ int32_t kv_place(const KvRows &x, int64_t r) {
 // A thread takes eight dimensions of a row's key: 8 contiguous numbers.  Of the value
 // it takes the same eight dimensions' single numbers, 4 tokens apart (a decode step);
 // where the batch has a block's four tokens in a row (prompts), it takes two of the
-// eight dimensions for all four, 8 contiguous numbers again.  Eight rows' threads lie
-// side by side, so that rows are read and keys are written 128 bytes at a time.
+// eight dimensions for all four, 8 contiguous numbers again.  A wave has eight rows'
+// threads side by side, so that rows are read and keys are written 128 bytes at a
+// time, and reads its rows' places and their neighbours' at once, beside its keys.
 template <typename P>
-__device__ inline void kv_write_eight(const KvRows &x, int64_t r, int32_t dim) {
+__global__ void __launch_bounds__(256) kv_write_kernel(KvRows x) {
     using T = typename P::T;
     using V8 = __attribute__((ext_vector_type(8))) T;
     union Eight {
@@ -414,52 +415,52 @@ __device__ inline void kv_write_eight(const KvRows &x, int64_t r, int32_t dim) {
         V8 v;
     } one;
     const KvView &c = x.c;
-    uint16_t in[8];
-    const int32_t p = kv_place(x, r), q = p & 3;
-    if (p < 0) return;
-    kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, in);
-    const int32_t head = (int32_t)((uint32_t)dim / (uint32_t)c.head_dim), d = dim - head * c.head_dim;
-    const int32_t t = p & (kv_page_tokens(c) - 1);
-    const int64_t page = p >> c.page_shift, lead = r - q;
-    const uint16_t *vrow = (const uint16_t *)x.v + dim;
-    bool whole = true;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) whole &= kv_place(x, lead + e) == p - q + e;
-
-    P::put(in, c.k_scale, one.e);
-    *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = one.v;
-
-    T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
-    if (whole) {
-        const int32_t two = 2 * q;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint16_t *src = vrow + (lead + e) * x.v_stride + two;
-            const uint32_t w = x.aligned ? *(const uint32_t *)src : src[0] | (uint32_t)src[1] << 16;
-            in[e] = (uint16_t)w;
-            in[4 + e] = (uint16_t)(w >> 16);
-        }
-        P::put(in, c.v_scale, one.e);
-        *(V8 *)(dst + 4 * two) = one.v;
-    } else {
-        kv_load8(vrow + r * x.v_stride, x.aligned, in);
-        P::put(in, c.v_scale, one.e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dst[4 * i + q] = one.e[i];
-    }
-}
-
-template <typename P>
-__global__ void __launch_bounds__(256) kv_write_kernel(KvRows x) {
-    const uint32_t eights = (uint32_t)(x.c.kv_heads * x.c.head_dim / 8);
-    const uint64_t items = (uint64_t)(x.rows + 7) / 8 * 8 * eights;
+    const int32_t width = c.kv_heads * c.head_dim, lane = (int32_t)(threadIdx.x & 63);
+    const uint32_t waves = ((uint32_t)width / 8 + 7) / 8;  // of a set of eight rows
+    const uint64_t items = (uint64_t)(x.rows + 7) / 8 * waves;
     // Workgroup b runs on XCD b % 8: neighbouring rows, whose tokens share cache lines,
     // go to the same one.  The grid is in eights.
     const uint64_t each = gridDim.x / 8, b = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    for (uint64_t id = b * 256 + threadIdx.x; id < items; id += 8 * each * 256) {
-        const uint64_t set = items < (1ull << 32) ? (uint32_t)id / (8 * eights) : id / (8 * eights);
-        const uint32_t in = (uint32_t)(id - set * (8 * eights));
-        kv_write_eight<P>(x, (int64_t)(set * 8 + (in & 7)), (int32_t)(in >> 3) * 8);
+    for (uint64_t id = b * 4 + (threadIdx.x >> 6); id < items; id += 8 * each * 4) {
+        const uint64_t set = items < (1ull << 32) ? (uint32_t)id / waves : id / waves;
+        const int32_t dim = ((int32_t)(id - set * waves) * 8 + (lane >> 3)) * 8, near = 4 + (lane & 7);
+        const int64_t r = (int64_t)set * 8 + (lane & 7);
+        const bool in = dim < width && r < x.rows;
+        const int32_t places = kv_place(x, (int64_t)set * 8 - 4 + (lane & 15));
+        uint16_t key[8], val[8];
+        if (in) kv_load8((const uint16_t *)x.k + r * x.k_stride + dim, x.aligned, key);
+        const int32_t p = __shfl(places, near), q = p & 3;
+        bool whole = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) whole &= __shfl(places, near - q + e) == p - q + e;
+        if (!in || p < 0) continue;
+
+        const int32_t head = (int32_t)((uint32_t)dim / (uint32_t)c.head_dim), d = dim - head * c.head_dim;
+        const int32_t t = p & (kv_page_tokens(c) - 1);
+        const int64_t page = p >> c.page_shift;
+        const uint16_t *vrow = (const uint16_t *)x.v + r * x.v_stride + dim;
+        const int32_t two = 2 * q;
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint16_t *src = vrow + (e - q) * x.v_stride + two;
+                const uint32_t w = x.aligned ? *(const uint32_t *)src : src[0] | (uint32_t)src[1] << 16;
+                val[e] = (uint16_t)w;
+                val[4 + e] = (uint16_t)(w >> 16);
+            }
+        } else {
+            kv_load8(vrow, x.aligned, val);
+        }
+        P::put(key, c.k_scale, one.e);
+        *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = one.v;
+        P::put(val, c.v_scale, one.e);
+        T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
+        if (whole) {
+            *(V8 *)(dst + 4 * two) = one.v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dst[4 * i + q] = one.e[i];
+        }
     }
 }
 

@@ -171,12 +171,13 @@ int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window,
     a->group = group;
     a->q_heads = q_heads;
     // Few sequences that cannot be long: a workgroup of many waves each, and nothing to
-    // join.  That takes less than a split where a wave has two tiles (one sequence of 611
-    // tokens, 14 heads of 64: 6.5 us, split 8.6; of 2,000: 10.4 and 8.8), or where the
-    // workgroups fill the GPU anyway (32 of 500 to 1,500 on 8 key heads of 128: 25.7, 30.0).
+    // join.  That takes less than shares where a wave has a few tiles (one sequence of 611
+    // tokens, 14 heads of 64: 6.0 us, in shares 8.1; of 1,000: 7.5 and 8.3; of 2,000: 10.7
+    // and 8.3; 8 of 500 on 4 key heads of 256: 13.2 and 11.7), or where the workgroups fill
+    // the GPU anyway (32 of 500 to 1,500 on 8 key heads of 128: 24.2, 30.0).
     const int64_t pairs = n * c->kv_heads * ((group + 15) / 16);
-    const int32_t step = pr::kv_wide(c->head_dim) * pr::kKvTile;
-    a->wide = pairs <= kComputeUnits && span <= (pairs * 2 > kComputeUnits ? 8 : 2) * step;
+    const int32_t step = pr::kKvWideWaves * pr::kKvTile, few = c->head_dim <= 128 ? 4 : 1;
+    a->wide = pairs <= kComputeUnits && span <= (pairs * 2 > kComputeUnits ? 8 : few) * step;
     const int32_t rows = a->wide ? 1 : pr::kv_rows(group, c->head_dim);
     a->row_groups = (group + 16 * rows - 1) / (16 * rows);
     const int32_t heads = c->kv_heads * a->row_groups;
@@ -302,7 +303,7 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
     const bool aligned = !((((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) || (rows > 1 && (k_stride | v_stride) & 7));
     const pr::KvRows x{view(c), place, k_rows, v_rows, k_stride, v_stride, rows, layer, aligned};
     hipStream_t st = (hipStream_t)hip_stream;
-    const unsigned grid = (blocks((rows + 7) / 8 * 8 * (width / 8), kMostGrid - 7) + 7) / 8 * 8;
+    const unsigned grid = (blocks((rows + 7) / 8 * ((width + 63) / 64) * 64, kMostGrid - 7) + 7) / 8 * 8;
     if (c->dtype != PR_KV_E4M3) pr::kv_write_kernel<pr::KvSame><<<grid, 256, 0, st>>>(x);
     else if (io == PR_KV_BF16) pr::kv_write_kernel<pr::KvE4m3<true>><<<grid, 256, 0, st>>>(x);
     else pr::kv_write_kernel<pr::KvE4m3<false>><<<grid, 256, 0, st>>>(x);

@@ -54,8 +54,9 @@ static void one(std::mt19937 &rng) {
             for (int t = from + kKvTile * wave; t < to; t += kKvTile * waves)
                 for (int h = 0; h < 2; ++h) {
                     const int tok = t + 16 * h;
-                    if (tok < to) CHECK((tok >> c.page_shift) < c.slot_pages);  // the table entry that is read
-                    const int pg = tok < to ? table[tok >> c.page_shift] : -1;
+                    // the table entry that is read: of a page of the row's, whatever the length
+                    CHECK(tok >= room || (tok >> c.page_shift) < c.slot_pages);
+                    const int pg = tok < room ? table[tok >> c.page_shift] : -1;
                     const bool good = kv_page_ok(c, pg);
                     for (int lane = 0; lane < 64; ++lane) {
                         const int col = lane & 15, g = lane >> 4;

@@ -138,6 +138,25 @@ def test_attend_split_lengths(kind, io):
     _attend_case(kind, 128, 64, 2, 4, [3000, 1, 0, 5000, 255, 256, 257, 512, 513, 1025], io=_types()[io] if io else None)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("group", [3, 20])
+def test_attend_shares(kind, dim, group):
+    """Tables with room for long sequences: shares that end inside sequences, go on to the next ones and meet empty
+    ones, for one sixteen of query heads and for two."""
+    _attend_case(kind, dim, 16, 2, group, [2000, 1, 0, 0, 700, 129, 128, 127, 0, 3000, 0], slot_pages=500)
+    _attend_case(kind, dim, 32, 1, group, [1500, 0, 40], window=600, slot_pages=300)
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 128, 129, 256, 257, 600])
+def test_attend_batch_sizes(n):
+    """Batches around the sizes where a wave looks through another 64 lengths, and past which a launch of its own
+    does; most sequences short, so that with 16 key heads shares keep to them."""
+    lengths = [(37 * i) % 300 for i in range(n)]
+    _attend_case("bf16", 64, 16, 1, 2, lengths, slot_pages=100)
+    _attend_case("fp16", 64, 16, 16, 1, lengths[:-1] + [1300], slot_pages=100)
+
+
 def test_attend_one_long_sequence_and_many_short_ones():
     _attend_case("bf16", 64, 16, 1, 8, [40000])
     _attend_case("bf16", 64, 16, 1, 2, [17] * 300 + [3000] + [0] * 20)  # more entries than a wave looks through
