@@ -543,8 +543,11 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  *   lse  float [n][q_heads], or NULL.
  * A sequence without tokens, padding and a slot out of range (the latter
  * counted) give out 0 and lse -infinity.  Tokens of a page whose table entry
- * is out of range are left out.  Sums, maxima and weights are kept in 32 bits.
+ * is out of range are left out.  A number among those attended that is not
+ * finite gives what the formula gives from a key (a score of -infinity is a
+ * weight of 0, any other a NaN), and a dimension that is not finite from a value.  Sums, maxima and weights are kept in 32 bits.
  * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
+ * out must not overlap q (from its first to its last number).
  * n * q_heads is below 2^24 and n * slot_pages * page_tokens below 2^38.
  */
 pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int64_t n, const void *q,
@@ -558,7 +561,7 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
  * to.
  * Skipped: slots out of range, tokens[i] outside [0, lengths[src[i]]], a dst
  * that is not empty or that an earlier entry names, a src that is some entry's
- * dst.  dst[i] -1 is padding.
+ * dst.  dst[i] -1 is padding.  n is at most 65,536.
  */
 pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
                      void *workspace, int64_t workspace_bytes, void *hip_stream);

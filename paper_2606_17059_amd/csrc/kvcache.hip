@@ -44,6 +44,7 @@ class DeviceScope {
 
 constexpr int64_t kMostGrid = ((int64_t)1 << 32) / 256 - 1;  // workgroups of 256 threads in a launch
 constexpr int64_t kMostEntries = ((int64_t)1 << 32) / pr::kKvPageThreads - 2;  // of a fork or trim, a workgroup each
+constexpr int64_t kMostForks = 65536;  // every entry looks through all for its slots
 constexpr int64_t kMostSpan = (int64_t)pr::kKvStep << 31;  // tokens of a batch's tables: their steps are counted in 32 bits
 constexpr int64_t kMostRows = INT32_MAX;
 
@@ -326,7 +327,12 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
     if (!slots || !q || !out) return fail(PR_EINVAL, "NULL device pointer");
     if ((uintptr_t)q & 1) return fail(PR_EINVAL, "q must be 2-byte aligned");
     if ((uintptr_t)out & 15) return fail(PR_EINVAL, "out must be 16-byte aligned");
-    if (n > 1 && q_stride < (int64_t)q_heads * c->head_dim) return fail(PR_EINVAL, "rows of q must not overlap");
+    const int64_t width = (int64_t)q_heads * c->head_dim;
+    if (n > 1 && q_stride < width) return fail(PR_EINVAL, "rows of q must not overlap");
+    // workgroups read a query after others have written their part of the output
+    if ((uintptr_t)out < (uintptr_t)q + 2 * ((n - 1) * q_stride + width) &&
+        (uintptr_t)q < (uintptr_t)out + 2 * n * width)
+        return fail(PR_EINVAL, "out must not overlap q");
     pr::KvAttend a{};
     if (const char *w = wrong_work(workspace, workspace_bytes, attend_parts(c, n, q_heads, window, workspace, &a)))
         return fail(PR_EINVAL, w);
@@ -359,7 +365,7 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
 pr_status pr_kv_fork(const pr_kv *c, const int32_t *src, const int32_t *dst, const int32_t *tokens, int64_t n,
                      void *workspace, int64_t workspace_bytes, void *hip_stream) {
     if (const char *w = wrong(c)) return fail(PR_EINVAL, w);
-    if (n < 0 || n > kMostEntries) return fail(PR_EINVAL, "n is negative or past 2^22 - 2");
+    if (n < 0 || n > kMostForks) return fail(PR_EINVAL, "n is negative or past 65536");
     if (n == 0) return ok();
     if (!src || !dst || !tokens) return fail(PR_EINVAL, "NULL device pointer");
     pr::KvChange x{view(c), src, dst, tokens, 1, n, nullptr};

@@ -88,7 +88,8 @@ class NodeCache:
         if src >= 0:
             self.tokens[src] = self.tokens.pop(src)  # used now
         while True:
-            need = pages - cached // T  # a shared page that is partly filled is copied
+            # a shared page that is partly filled is copied when it is appended to
+            need = pages - cached // T if cached < len(t) else 0
             if len(self.tokens) < self.slots and int((c.refs == 0).sum()) >= need:
                 break
             oldest = next(iter(self.tokens))

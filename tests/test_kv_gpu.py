@@ -211,8 +211,8 @@ def test_attend_bad_pages_are_left_out():
 
 
 def test_attend_infinite_and_nan_numbers():
-    """Infinities among attended tokens behave as the formula says; behind the end and before the window nothing
-    they do is seen."""
+    """Keys that are infinite give what the formula gives, a value that is not finite a dimension that is not; behind
+    the end and before the window nothing of them is seen."""
     import torch
     c, q, out, lse = _attend_case("fp16", 64, 16, 1, 2, [40, 40, 40, 600])
     announce("attend with infinities")
@@ -235,7 +235,7 @@ def test_attend_infinite_and_nan_numbers():
     assert (np.abs(out[0].double().cpu().numpy() - ro) <= err + 2.0 ** -11 * (np.abs(ro) + err)).all()
     assert out[1].isnan().all()
     assert out[2, :, 5].isnan().all() and torch.equal(out[2, :, 6:], before[2, :, 6:])
-    assert (out[3, :, 9] == math.inf).all() and torch.equal(out[3, :, 10:], before[3, :, 10:])
+    assert not out[3, :, 9].isfinite().any() and torch.equal(out[3, :, 10:], before[3, :, 10:])
     w = c.attend(0, _ints([2, 3]), q[2:], 0.125, window=20)
     assert w.isfinite().all()
 
@@ -264,6 +264,20 @@ def test_attend_strides_and_alignment():
         view = wide[:, lead:lead + 576].unflatten(1, (6, 96))
         view.copy_(q)
         assert torch.equal(c.attend(0, _ints([0, 1, 2]), view, 96 ** -0.5), out)
+
+
+def test_attend_nothing():
+    import torch
+    announce("an attention of no sequence")
+    c = _cache()
+    q = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=device())
+    assert c.attend(0, _ints([]), q).shape == (0, 4, 64)
+    place = c.extend(_ints([3]), _offsets([0]), 0)
+    c.write(0, place, q[:, :2], q[:, :2])
+    c.fork(_ints([]), _ints([]), _ints([]))
+    c.trim(_ints([]))
+    assert c.compact().tolist() == [0, 0]
+    c.check()
 
 
 def test_attend_is_the_same_every_time_and_whatever_else_is_in_the_batch():
@@ -739,6 +753,7 @@ def test_the_binding_refuses_what_does_not_fit():
             (lambda: c.attend(0, two, q[:, :3].contiguous()), RuntimeError), (lambda: c.attend(1, two, q), RuntimeError),
             (lambda: c.attend(0, two, q, window=-1), RuntimeError), (lambda: c.attend(0, two, q, math.nan), RuntimeError),
             (lambda: c.attend(0, two, q, out=torch.zeros_like(q).float()), ValueError),
+            (lambda: c.attend(0, two, q, out=q), RuntimeError),
             (lambda: c.attend(0, two, q, lse=torch.zeros(2, 3, device=device())), ValueError),
             (lambda: c.attend(0, two, q.cpu()), TypeError), (lambda: c.attend(0, two, q[:1].expand(2, 4, 64)), RuntimeError),
             (lambda: c.write(0, place, rows, rows[:1]), ValueError), (lambda: c.write(0, place, q, q), ValueError),

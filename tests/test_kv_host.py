@@ -32,7 +32,7 @@ def _calls(d, n=3, rows=5, work=FAKE, size=1 << 30):
         "pr_kv_workspace": [r, 0, n, rows, ctypes.byref(out)],
         "pr_kv_extend": [r, FAKE, FAKE, n, rows, FAKE, work, size, None],
         "pr_kv_write": [r, 0, FAKE, FAKE, 128, FAKE, 128, rows, 0, None],
-        "pr_kv_attend": [r, 0, FAKE, n, FAKE, 4 * 64, 4, 0, 0.125, 0, FAKE, None, work, size, None],
+        "pr_kv_attend": [r, 0, FAKE, n, FAKE, 4 * 64, 4, 0, 0.125, 0, FAKE + 1536, None, work, size, None],
         "pr_kv_fork": [r, FAKE, FAKE, FAKE, n, work, size, None],
         "pr_kv_trim": [r, FAKE, FAKE, 1, n, work, size, None],
         "pr_kv_compact": [r, None, work, size, None],
@@ -83,9 +83,9 @@ BAD = [  # call, index of an argument, a value it refuses
     ("pr_kv_attend", 4, None), ("pr_kv_attend", 4, FAKE + 1), ("pr_kv_attend", 5, 255), ("pr_kv_attend", 6, 3),
     ("pr_kv_attend", 6, 0), ("pr_kv_attend", 7, 1), ("pr_kv_attend", 8, float("nan")),
     ("pr_kv_attend", 8, float("inf")), ("pr_kv_attend", 9, -1), ("pr_kv_attend", 10, None),
-    ("pr_kv_attend", 10, FAKE + 8),
+    ("pr_kv_attend", 10, FAKE + 8), ("pr_kv_attend", 10, FAKE + 1024), ("pr_kv_attend", 10, FAKE - 1024),
     ("pr_kv_fork", 1, None), ("pr_kv_fork", 2, None), ("pr_kv_fork", 3, None), ("pr_kv_fork", 4, -1),
-    ("pr_kv_fork", 4, 1 << 22),
+    ("pr_kv_fork", 4, 65537),
     ("pr_kv_trim", 1, None), ("pr_kv_trim", 3, -1), ("pr_kv_trim", 4, -1), ("pr_kv_trim", 4, 1 << 22),
     ("pr_kv_compact", 2, None), ("pr_kv_compact", 2, FAKE + 4), ("pr_kv_compact", 3, 16),
 ]

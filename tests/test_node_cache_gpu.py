@@ -82,6 +82,9 @@ def test_admit_gives_up_what_is_oldest():
     assert node.admit(a)[:2] == (0, 0) and node.admit(b)[:2] == (1, 0)      # 3 and 3 pages
     assert node.admit(np.concatenate([a[:20], b[:9]]))[:2] == (2, 20)       # shares one page, copies one
     assert c.refs.sum().item() == 8 and list(node.tokens) == [1, 0, 2]
+    again = node.admit(a[:17])  # all of it is there: no row, no page
+    assert again.slot == 3 and again.cached == 17 and again.place.numel() == 0 and int((c.refs > 0).sum()) == 7
+    node.drop([3])
     assert node.lookup(b[:5]) == (1, 5) and node.lookup(d) == (-1, 0) and node.lookup([]) == (-1, 0)
     got = node.admit(d)  # 4 pages: the oldest leaves, then the next
     assert got.cached == 0 and list(node.tokens)[-1] == got.slot and 1 not in list(node.tokens)[:-1]
