@@ -468,8 +468,8 @@ pr_status pr_forest_host_image(pr_forest *f, pr_image_view *out);
 typedef struct {
     int32_t device;      /* HIP device of every pointer below */
     int32_t dtype;       /* of k and v: PR_KV_BF16, PR_KV_F16 or PR_KV_E4M3 */
-    int32_t layers;      /* >= 1 */
-    int32_t kv_heads;    /* >= 1 */
+    int32_t layers;      /* >= 1, layers * kv_heads <= 2^30 */
+    int32_t kv_heads;    /* >= 1, a page below 2^31 bytes */
     int32_t head_dim;    /* 64, 96, 128, 192 or 256 */
     int32_t page_tokens; /* 16, 32, 64, 128 or 256 */
     int32_t num_pages;   /* >= 1, num_pages * page_tokens < 2^31 */

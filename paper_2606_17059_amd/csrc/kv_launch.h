@@ -34,13 +34,13 @@ struct KvAttend {
 
 // Sixteens of query heads ("rows") a workgroup takes: two share the keys and values
 // that one would read twice, but past 128 dimensions two rows' output leaves room
-// for one wave a SIMD, which loses more (48 rows of 192 dimensions, e4m3: 60 us with
-// one, 86 with two).
+// for one wave a SIMD, which loses more (48 rows of 192 dimensions, e4m3: 52 us with
+// one, 72 with two, 58 with three).
 constexpr int kv_rows(int group, int head_dim) { return group > 16 && head_dim <= 128 ? 2 : 1; }
 
 // Waves a SIMD holds of the attention kernel, by its registers (and, of a workgroup
 // of many waves, at least its own).  One for 256 dimensions in 16 bits: two would
-// spill (64 sequences of 2,000 tokens, 4 key heads: 112 us with one, 124 with two).
+// spill (64 sequences of 2,000 tokens, 4 key heads: 97 us with one, 119 with two).
 constexpr int kv_resident(bool e4m3, int head_dim, int rows, int waves) {
     const int n = head_dim * rows;
     const int many = e4m3 ? (n <= 64 ? 5 : (n <= 128 ? 4 : (n <= 192 ? 3 : 2)))

@@ -84,7 +84,7 @@ PR_KV_FN uint32_t kv_share(uint32_t steps, const KvSplit &s) {
 // longer than a share.  So it is where there are more sequences than shares and they
 // are short: a share of several would begin anew with each, where workgroups beside it
 // could (600 sequences of 10 to 600 tokens on 4 key heads of 128: 82 us, 87 across;
-// 128 of 4,096 to 16,384 on 8: 935 us, 910 across).
+// 128 of 4,096 to 16,384 on 8: 953 us, 904 across).
 constexpr uint32_t kKvShort = 8;   // steps of a short sequence, on average
 PR_KV_FN bool kv_keeps(uint32_t steps, int64_t n, const KvSplit &s) { return n >= s.fill && steps < n * kKvShort; }
 PR_KV_FN uint32_t kv_even(uint32_t steps, uint32_t shares) { return (steps + shares - 1) / shares; }

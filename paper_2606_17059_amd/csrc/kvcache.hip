@@ -65,6 +65,7 @@ const char *wrong(const pr_kv *c) {
     if (!c->k || !c->v || !c->table || !c->lengths || !c->refs || !c->free_pages || !c->skipped)
         return "pr_kv has a NULL pointer";
     if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return "k and v must be 16-byte aligned";
+    if ((int64_t)c->layers * c->kv_heads > (1 << 30)) return "layers * kv_heads must be at most 2^30";
     const int64_t unit = 16 / element_bytes(c), page = (int64_t)c->kv_heads * d * t;
     if (c->kv_heads > (1 << 20) || page * 2 > INT32_MAX) return "a page must be smaller than 2^31 bytes";
     for (const int64_t s : {c->k_layer, c->k_page, c->v_layer, c->v_page})
@@ -162,8 +163,8 @@ int64_t compact_parts(const pr_kv *c, void *work, pr::KvCompact *x) {
 
 constexpr int kComputeUnits = 256;
 
-// The parts of an attention's split that go by the host's numbers (a.window and
-// the cache's sizes among them), and its workspace.
+// How an attention is split, as far as that goes by the host's numbers, and its
+// workspace.
 int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window, void *work, pr::KvAttend *a) {
     const bool e4m3 = c->dtype == PR_KV_E4M3;
     const int32_t group = q_heads / c->kv_heads;

@@ -44,7 +44,7 @@ def _calls(d, n=3, rows=5, work=FAKE, size=1 << 30):
     dict(dtype=3), dict(dtype=-1), dict(device=-1), dict(layers=0), dict(kv_heads=0), dict(head_dim=80),
     dict(head_dim=512), dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=512), dict(num_pages=0),
     dict(num_slots=0), dict(slot_pages=0), dict(num_pages=1 << 27), dict(slot_pages=(1 << 26) + 1), dict(k=None),
-    dict(v=FAKE + 8), dict(table=None), dict(lengths=None), dict(refs=None), dict(free_pages=None),
+    dict(layers=1 << 30), dict(kv_heads=1 << 21), dict(v=FAKE + 8), dict(table=None), dict(lengths=None), dict(refs=None), dict(free_pages=None),
     dict(skipped=None), dict(k_page=2044), dict(k_page=2040), dict(v_layer=-8), dict(v_layer=2040),
     dict(k_scale=0.5), dict(v_scale=float("nan")), dict(dtype=2, k_scale=0.0), dict(dtype=2, v_scale=float("inf")),
     dict(dtype=2, k_page=2056), None])
