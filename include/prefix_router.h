@@ -474,7 +474,7 @@ typedef struct {
     int32_t page_tokens; /* 16, 32, 64, 128 or 256 */
     int32_t num_pages;   /* >= 1, num_pages * page_tokens < 2^31 */
     int32_t num_slots;   /* >= 1 */
-    int32_t slot_pages;  /* pages a sequence may have, >= 1, slot_pages * page_tokens < 2^31 */
+    int32_t slot_pages;  /* pages a sequence may have, >= 1, slot_pages * page_tokens <= 2^30 */
     float k_scale;       /* PR_KV_E4M3: finite and positive; else 1 */
     float v_scale;
     void *k, *v;         /* 16-byte aligned */
@@ -499,7 +499,8 @@ pr_status pr_kv_init(const pr_kv *c, void *hip_stream);
 #define PR_KV_WORK_CHANGE 3  /* a fork or trim of n entries; m is 0 */
 
 /* Bytes (HOST, *bytes) of workspace that a call with these sizes needs (0: none,
- * and its workspace may be NULL). */
+ * and its workspace may be NULL).  An attend of fewer entries can need more: a
+ * workspace for several sizes is as large as the largest of their answers. */
 pr_status pr_kv_workspace(const pr_kv *c, int32_t call, int64_t n, int64_t m, int64_t *bytes);
 
 /*
@@ -526,7 +527,8 @@ pr_status pr_kv_extend(const pr_kv *c, const int32_t *slots, const int64_t *offs
  * PR_KV_F16: the cache's own, or either for a PR_KV_E4M3 cache, which takes the
  * nearest of its values to number / scale, ties to even, +-448 past its range,
  * NaN for NaN.  Rows whose place is negative or past the last page are left
- * out (not counted).
+ * out (not counted).  A place that occurs twice gets the numbers of one of its
+ * rows, or of each in part.
  */
 pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const void *k_rows, int64_t k_stride,
                       const void *v_rows, int64_t v_stride, int64_t rows, int32_t io, void *hip_stream);
@@ -545,7 +547,10 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  * counted) give out 0 and lse -infinity.  Tokens of a page whose table entry
  * is out of range are left out.  A number among those attended that is not
  * finite gives what the formula gives from a key (a score of -infinity is a
- * weight of 0, any other a NaN), and a dimension that is not finite from a value.  Sums, maxima and weights are kept in 32 bits.
+ * weight of 0, any other a NaN), and a dimension that is not finite from a
+ * value.  A row all of whose weights are 0 is one without tokens.  Sums, maxima
+ * and weights are kept in 32 bits: values up to 2^88 cannot overflow them.
+ * scale and scale * k_scale have to be finite.
  * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
  * out must not overlap q (from its first to its last number).
  * n * q_heads is below 2^24 and n * slot_pages * page_tokens below 2^38.

@@ -105,17 +105,15 @@ struct KvShare {
     uint32_t begin, end, size, first, index;
     int32_t entry;
 };
-__device__ __forceinline__ KvShare kv_share_of(uint32_t u, uint32_t size, uint32_t steps) {
-    KvShare r{u * size, 0, size, 0, u, -1};
+__device__ __forceinline__ KvShare kv_share_of(uint32_t u, uint32_t size, uint32_t steps, const KvSplit &s) {
+    KvShare r{kv_share_begin(u, size, steps, s), steps, size, 0, u, -1};
     r.end = min(r.begin + size, steps);
     return r;
 }
 // Share k of an entry's own.
 __device__ __forceinline__ KvShare kv_own_share(int32_t entry, uint32_t steps, uint32_t shares, uint32_t k) {
-    KvShare r = kv_share_of(k, kv_even(steps, shares), steps);
-    r.index = 0;
-    r.entry = entry;
-    return r;
+    const uint32_t size = kv_even(steps, shares);
+    return KvShare{k * size, min((k + 1) * size, steps), size, 0, 0, entry};
 }
 
 // Share u of a batch of at most E * 64 entries, found by every wave for itself from
@@ -159,7 +157,7 @@ __device__ inline KvShare kv_find_share(const KvAttend &a, uint32_t u) {
     add();
     const uint32_t size = kv_share(total, a.split);
     if (!kv_keeps(total, a.n, a.split)) {
-        KvShare r = kv_share_of(u, size, total);
+        KvShare r = kv_share_of(u, size, total, a.split);
         find(r.begin);
         r.entry = entry;
         r.first = before;
@@ -188,7 +186,7 @@ __device__ inline KvShare kv_planned_share(const KvAttend &a, uint32_t u) {
     Scalar *before = scalar(a.plan);
     const uint32_t total = (uint32_t)before[a.n];
     const bool keeps = kv_keeps(total, a.n, a.split);
-    KvShare r = kv_share_of(u, kv_share(total, a.split), total);
+    KvShare r = kv_share_of(u, kv_share(total, a.split), total, a.split);
     Scalar *sums = keeps ? before + a.n + 1 : before;
     const uint32_t v = keeps ? u : r.begin;
     if (v >= (uint32_t)sums[a.n]) return r;
@@ -528,8 +526,8 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
                 if (done.whole) {
                     const int64_t to_row = (int64_t)done.entry * a.q_heads + at;
                     if (a.lse && j == 0 && g == 0)
-                        a.lse[to_row] = done.length ? (most + log2f(sum)) * 0.6931471805599453f : -INFINITY;
-                    const float unit_v = done.length ? c.v_scale / sum : 0.f;
+                        a.lse[to_row] = (most + log2f(sum)) * 0.6931471805599453f;
+                    const float unit_v = sum == 0.f ? 0.f : c.v_scale / sum;  // 0: no token counts
                     *(u32x4 *)((uint32_t *)a.out + (to_row * D + 32 * j + 8 * g) / 2) =
                         u32x4{IO::pack(u[0] * unit_v, v[0] * unit_v), IO::pack(u[1] * unit_v, v[1] * unit_v),
                               IO::pack(u[2] * unit_v, v[2] * unit_v), IO::pack(u[3] * unit_v, v[3] * unit_v)};
@@ -622,7 +620,7 @@ __global__ void __launch_bounds__(kv_join_threads(D, MANY)) kv_join_kernel(KvAtt
     if (!in) return;
     const int64_t to_row = entry * a.q_heads + row;
     if (a.lse && col == 0) a.lse[to_row] = (m + log2f(l)) * 0.6931471805599453f;
-    const float unit_v = a.c.v_scale / l;
+    const float unit_v = l == 0.f ? 0.f : a.c.v_scale / l;
     *(u32x2 *)((uint32_t *)a.out + (to_row * D + 4 * col) / 2) =
         u32x2{IO::pack(o[0] * unit_v, o[1] * unit_v), IO::pack(o[2] * unit_v, o[3] * unit_v)};
 }

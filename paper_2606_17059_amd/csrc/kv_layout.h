@@ -79,6 +79,11 @@ PR_KV_FN uint32_t kv_share(uint32_t steps, const KvSplit &s) {
     const uint32_t c = (steps + s.fill - 1) / s.fill;
     return c < s.least ? s.least : c;
 }
+// First step of share u, `steps` where there is none.  Shares from `fill` on have
+// nothing, and their product may pass 32 bits.
+PR_KV_FN uint32_t kv_share_begin(uint32_t u, uint32_t size, uint32_t steps, const KvSplit &s) {
+    return u < s.fill ? u * size : steps;
+}
 
 // Whether shares keep to sequences instead: one for each, or equal ones of a sequence
 // longer than a share.  So it is where there are more sequences than shares and they

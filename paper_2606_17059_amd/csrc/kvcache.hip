@@ -347,6 +347,7 @@ pr_status pr_kv_attend(const pr_kv *c, int32_t layer, const int32_t *slots, int6
     a.layer = layer;
     a.window = window;
     a.scale = (float)((double)scale * c->k_scale * 1.4426950408889634);
+    if (!std::isfinite(a.scale)) return fail(PR_EINVAL, "scale times k_scale must be finite");
     a.q_aligned = !((uintptr_t)q & 15) && (n == 1 || !(q_stride & 7));
     if (((int64_t)a.units * c->kv_heads + 7) / 8 * 8 * a.row_groups > kMostGrid)
         return fail(PR_EINVAL, "the batch has too many entries and key heads");

@@ -141,7 +141,7 @@ static void split(std::mt19937 &rng) {
         }
     } else {
         for (int64_t u = 0; u < units; ++u) {
-            const uint32_t begin = (uint32_t)u * c, end = std::min(begin + c, first[n]);
+            const uint32_t begin = kv_share_begin((uint32_t)u, c, first[n], s), end = std::min(begin + c, first[n]);
             if (begin >= first[n]) continue;
             int i = 0;
             while (first[i + 1] <= begin) ++i;
@@ -167,10 +167,30 @@ static void split(std::mt19937 &rng) {
     for (int x : used) CHECK(x <= 1);
 }
 
+// Shares of the most steps and the most workgroups that a batch may have: each step is
+// in one share, though the last workgroups' products pass 32 bits.
+static void many() {
+    for (const uint32_t fill : {1u, 2u, 7u, 1280u})
+        for (const uint32_t steps : {1u << 19, 1u << 27, (1u << 31) + 5})
+            for (const uint32_t n : {1u, fill, 1u << 16, 1u << 23}) {
+                const KvSplit s{fill, 4};
+                const uint32_t c = kv_share(steps, s);
+                uint32_t covered = 0;
+                for (uint32_t u = 0; u < fill + n; ++u) {
+                    const uint32_t begin = kv_share_begin(u, c, steps, s);
+                    if (begin >= steps) continue;
+                    CHECK(begin == covered && begin + c > begin);
+                    covered = std::min(begin + c, steps);
+                }
+                CHECK(covered == steps);
+            }
+}
+
 int main() {
     std::mt19937 rng(7);
     for (int i = 0; i < 300; ++i) one(rng);
     for (int i = 0; i < 3000; ++i) split(rng);
+    many();
     printf("kv_addresses: %s\n", failures ? "failed" : "ok");
     return failures != 0;
 }

@@ -82,7 +82,7 @@ BAD = [  # call, index of an argument, a value it refuses
     ("pr_kv_attend", 1, 2), ("pr_kv_attend", 2, None), ("pr_kv_attend", 3, -1), ("pr_kv_attend", 3, 1 << 24),
     ("pr_kv_attend", 4, None), ("pr_kv_attend", 4, FAKE + 1), ("pr_kv_attend", 5, 255), ("pr_kv_attend", 6, 3),
     ("pr_kv_attend", 6, 0), ("pr_kv_attend", 7, 1), ("pr_kv_attend", 8, float("nan")),
-    ("pr_kv_attend", 8, float("inf")), ("pr_kv_attend", 9, -1), ("pr_kv_attend", 10, None),
+    ("pr_kv_attend", 8, float("inf")), ("pr_kv_attend", 8, 3e38), ("pr_kv_attend", 9, -1), ("pr_kv_attend", 10, None),
     ("pr_kv_attend", 10, FAKE + 8), ("pr_kv_attend", 10, FAKE + 1024), ("pr_kv_attend", 10, FAKE - 1024),
     ("pr_kv_fork", 1, None), ("pr_kv_fork", 2, None), ("pr_kv_fork", 3, None), ("pr_kv_fork", 4, -1),
     ("pr_kv_fork", 4, 65537),
@@ -99,6 +99,15 @@ def test_a_bad_argument_is_refused(name, index, value):
     args[index] = value
     assert getattr(R.lib(), name)(*args) == R.PR_EINVAL
     assert R.pr_last_error()
+
+
+def test_a_score_scale_past_float_is_refused():
+    from paper_2606_17059_amd import router as R
+    d = _desc(dtype=2, k_scale=1e30)
+    args = _calls(d)["pr_kv_attend"]
+    args[8] = 1e10
+    assert R.lib().pr_kv_attend(*args) == R.PR_EINVAL
+    assert "scale times k_scale" in R.pr_last_error()
 
 
 def test_an_attention_that_splits_wants_its_workspace():
