@@ -74,7 +74,7 @@ class KVCache:
             self.k_scale, self.v_scale, k.data_ptr() or None, v.data_ptr() or None, *strides, table.data_ptr() or None, lengths.data_ptr() or None, refs.data_ptr() or None,
             free.data_ptr() or None, skipped.data_ptr())
         self._ref = ctypes.byref(self._desc)
-        self._index, self._int32, self._int64, self._uint8 = k.device.index, torch.int32, torch.int64, torch.uint8
+        self._torch, self._index, self._int32, self._int64 = torch, k.device.index, torch.int32, torch.int64
         # types that rows of new tokens and queries may have
         self._io = {torch.bfloat16: PR_KV_BF16, torch.float16: PR_KV_F16} if k.dtype.itemsize == 1 else \
             {k.dtype: codes[k.dtype]}
@@ -114,20 +114,19 @@ class KVCache:
             b = self._bytes[key] = out.value
         return b
 
-    def _empty(self, shape, dtype, stream):
-        """A tensor of the allocator's pool for the call's stream."""
-        torch = _load_torch()
+    def _empty(self, like, shape, stream):
+        """A tensor of `like`'s type, of the allocator's pool for the call's stream."""
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return like.new_empty(shape)
+        with self._torch.cuda.stream(stream):
+            return like.new_empty(shape)
 
     def _work(self, call: int, n: int, m: int, stream):
         """(a workspace or None, its address, its size)."""
         size = self._work_bytes(call, n, m)
         if not size:
             return None, None, 0
-        work = self._empty((size,), self._uint8, stream)
+        work = self._empty(self.lengths, (size + 3) // 4, stream)
         return work, work.data_ptr(), size
 
     def _st(self, stream) -> int:
@@ -178,7 +177,7 @@ class KVCache:
             raise ValueError("rows must not be negative")
         st = self._st(stream)
         if place is None:
-            place = self._empty((rows,), self._int32, stream)
+            place = self._empty(slots, rows, stream)
         else:
             self._ints(place, self._int32, "place", rows)
         work, at, size = self._work(PR_KV_WORK_EXTEND, n, rows, stream)
@@ -205,18 +204,17 @@ class KVCache:
         """Attention of one new token a sequence, q [n, heads, head_dim], over its cached tokens in one layer, or
         the last `window` of them (pr_kv_attend).  scale: 1 / sqrt(head_dim) unless given.  lse: a float32
         tensor [n, heads] that gets the logarithm of the sum of exponentials."""
-        torch = _load_torch()
         n = self._ints(slots, self._int32, "slots")
         heads, stride, io = self._rows(q, "q", n, 0)
         st = self._st(stream)
         if out is None:
-            out = self._empty((n, heads, self.head_dim), q.dtype, stream)
+            out = self._empty(q, q.shape, stream)
         elif out.dtype != q.dtype or tuple(out.shape) != tuple(q.shape) or not out.is_contiguous():
             raise ValueError("out must be a contiguous tensor of q's dtype and shape")
         elif out.device != self.device:
             raise ValueError("out must be on the cache's device")
         if lse is not None:
-            _dev(lse, torch.float32, "lse")
+            _dev(lse, self._torch.float32, "lse")
             if tuple(lse.shape) != (n, heads) or lse.device != self.device:
                 raise ValueError("lse must be [n, heads] on the cache's device")
         work, at, size = self._work(PR_KV_WORK_ATTEND, n, heads, stream)
@@ -243,7 +241,7 @@ class KVCache:
     def trim(self, slots, keep=None, stream=None) -> None:
         """Each slots[i] keeps its first keep[i] tokens, none without `keep` (pr_kv_trim).  keep may be a column of
         a route's match_len: a strided int32 vector."""
-        torch = _load_torch()
+        torch = self._torch
         n = self._ints(slots, self._int32, "slots")
         stride = 1
         if keep is not None:
@@ -263,7 +261,7 @@ class KVCache:
         """Move the held pages to the lowest ids; returns int32 [2] on the device: pages moved, pages held
         (pr_kv_compact)."""
         st = self._st(stream)
-        moved = self._empty((2,), self._int32, stream)
+        moved = self._empty(self.lengths, 2, stream)
         work, at, size = self._work(PR_KV_WORK_COMPACT, 0, 0, stream)
         s = self._lib.pr_kv_compact(self._ref, moved.data_ptr(), at, size, st)
         if s != PR_OK:
