@@ -219,7 +219,7 @@ class KVCache:
                 raise ValueError("lse must be [n, heads] on the cache's device")
         work, at, size = self._work(PR_KV_WORK_ATTEND, n, heads, stream)
         s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, stride,
-                                   heads, io, self._scale if scale is None else scale, window,
+                                   heads, io, self._scale if scale is None else scale, min(window, 0x7fffffff),
                                    out.data_ptr() or None, lse.data_ptr() or None if lse is not None else None,
                                    at, size, st)
         if s != PR_OK:

@@ -2,6 +2,7 @@
 tables and counts exactly, rows bit for bit, attention within what float32 sums
 and one rounding of the output allow."""
 import math
+import os
 
 import numpy as np
 import pytest
@@ -238,6 +239,15 @@ def test_attend_infinite_and_nan_numbers():
     assert not out[3, :, 9].isfinite().any() and torch.equal(out[3, :, 10:], before[3, :, 10:])
     w = c.attend(0, _ints([2, 3]), q[2:], 0.125, window=20)
     assert w.isfinite().all()
+
+
+def test_attend_a_window_past_every_length_is_none():
+    import torch
+    c, q, _, _ = _attend_case("bf16", 64, 16, 2, 2, [1, 40, 600])
+    announce("attend with wide windows")
+    want = c.attend(0, _ints(range(3)), q, 0.125)
+    for window in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 2 ** 40):
+        assert torch.equal(c.attend(0, _ints(range(3)), q, 0.125, window=window), want)
 
 
 def test_attend_all_scores_minus_infinity():
@@ -781,3 +791,21 @@ def test_the_binding_refuses_what_does_not_fit():
         c.trim(two)
         with pytest.raises(RuntimeError, match="capture"):
             c.check()
+
+
+def test_the_calls_from_c(tmp_path):
+    """tests/c/kv_check.c, plain C11 against the header and the built library."""
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    pkg, rocm = os.path.join(root, "paper_2606_17059_amd"), os.environ.get("ROCM_PATH", "/opt/rocm")
+    exe = str(tmp_path / "kv_check")
+    r = subprocess.run(["gcc", "-std=c11", "-Wall", "-Wextra", "-pedantic", "-Werror", "-D__HIP_PLATFORM_AMD__",
+                        "-isystem", os.path.join(rocm, "include"), "-I", os.path.join(root, "include"),
+                        os.path.join(root, "tests", "c", "kv_check.c"), "-o", exe, "-L", pkg, "-lprefix_router",
+                        "-Wl,-rpath," + pkg, "-L", os.path.join(rocm, "lib"), "-lamdhip64",
+                        "-Wl,-rpath," + os.path.join(rocm, "lib"), "-lm"],
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout
+    announce("KV cache from C")
+    r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
+    assert r.returncode == 0 and "kv_check: ok" in r.stdout, r.stdout
