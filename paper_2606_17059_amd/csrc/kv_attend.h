@@ -118,18 +118,21 @@ __device__ __forceinline__ KvShare kv_own_share(int32_t entry, uint32_t steps, u
 
 // Share u of a batch of at most E * 64 entries, found by every wave for itself from
 // the lengths: two loads and two dozen lane operations, about 1 us, where a launch
-// before this one that wrote the same down is 2.5 us and its work.
+// before this one that wrote the same down is 2.5 us and its work.  The loads have no
+// conditions, behind which each would be waited for before the next.
 template <int E>
 __device__ inline KvShare kv_find_share(const KvAttend &a, uint32_t u) {
     const int lane = (int)(threadIdx.x & 63);
-    int32_t slot[E];
+    int32_t slot[E], length[E];
     uint32_t mine[E], upto[E], total = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) slot[e] = e * 64 + lane < a.n ? a.slots[e * 64 + lane] : -1;
+    for (int e = 0; e < E; ++e) slot[e] = a.slots[min(e * 64 + lane, (int32_t)a.n - 1)];
+#pragma unroll
+    for (int e = 0; e < E; ++e) length[e] = kv_length(a.c, kv_slot_ok(a.c, slot[e]) ? slot[e] : 0);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int32_t length = kv_slot_ok(a.c, slot[e]) ? kv_length(a.c, slot[e]) : 0;
-        mine[e] = e * 64 + lane < a.n ? kv_steps(kv_span(length, a.window)) : 0;
+        if (!kv_slot_ok(a.c, slot[e])) length[e] = 0;
+        mine[e] = e * 64 + lane < a.n ? kv_steps(kv_span(length[e], a.window)) : 0;
     }
     auto add = [&] {
         total = 0;
@@ -245,20 +248,45 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     const int32_t uh = (int32_t)((blockIdx.x >> 3) / (unsigned)a.row_groups * 8 + (blockIdx.x & 7));
     const int32_t unit = (int32_t)((uint32_t)uh / (uint32_t)c.kv_heads), head = uh - unit * c.kv_heads;
     if (unit >= a.units) return;  // the grid is in eights
-    KvShare w{0, 1, 1, 0, 0, unit < a.n ? unit : -1};  // without a.where a share is an entry
-    if (a.plan) w = kv_planned_share(a, (uint32_t)unit);
-    else if (a.where) w = a.n <= 64    ? kv_find_share<1>(a, (uint32_t)unit)
-                          : a.n <= 128 ? kv_find_share<2>(a, (uint32_t)unit)
-                                       : kv_find_share<kKvScan / 64>(a, (uint32_t)unit);
-    if (w.entry < 0) return;
-    const uint32_t share_begin = (uint32_t)uniform((int)w.begin), share_end = (uint32_t)uniform((int)w.end);
-    uint32_t first = (uint32_t)uniform((int)w.first);
+    // Without a.where, and always in a workgroup of many waves, a share is an entry.
+    const bool shares = W == kKvWaves && a.where;
+    KvShare w{0, 1, 1, 0, 0, unit};
+    if (shares) {
+        if (a.plan) w = kv_planned_share(a, (uint32_t)unit);
+        else w = a.n <= 64    ? kv_find_share<1>(a, (uint32_t)unit)
+                 : a.n <= 128 ? kv_find_share<2>(a, (uint32_t)unit)
+                              : kv_find_share<kKvScan / 64>(a, (uint32_t)unit);
+        w.begin = (uint32_t)uniform((int)w.begin);
+        w.end = (uint32_t)uniform((int)w.end);
+        w.first = (uint32_t)uniform((int)w.first);
+        w.entry = uniform(w.entry);
+        if (w.entry < 0) return;
+    }
+    const uint32_t share_begin = w.begin, share_end = w.end;
+    uint32_t first = w.first;
     __shared__ f32x4 so[W][R * KB * 2][64];
     __shared__ float sm[W][R][16], sl[W][R][16];
 
     const int32_t row0 = rg * 16 * R, inside = kv_page_tokens(c) - 1, room = c.slot_pages << c.page_shift;
     const char *kbase = (const char *)c.k + SZ * (a.layer * c.k_layer + kv_head_base(c, head));
     const char *vbase = (const char *)c.v + SZ * (a.layer * c.v_layer + kv_head_base(c, head));
+
+    // A tile's page ids, and those of the wave's next tile, are `here` and `next`.
+    Scalar *pages = nullptr;
+    int32_t t = 0, here[2], next[2];
+    auto page_of = [&](int32_t tok) { return pages[min(tok, room - 1) >> c.page_shift]; };
+    auto first_pages = [&](int32_t slot) __attribute__((always_inline)) {
+        pages = scalar(c.table + (int64_t)slot * c.slot_pages);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            here[h] = page_of(t + 16 * h);
+            next[h] = page_of(t + kStep + 16 * h);
+        }
+    };
+    // Where a workgroup takes a whole sequence from its first token on, its first pages
+    // are known before its length, and are read beside it (one sequence of 611 tokens:
+    // 5.4 us, 5.8 with one after the other).
+    const bool whole = !shares && !a.window;
 
     // The share's part of entry i, whose first step is the batch's step `first`.
     auto part_of = [&](int32_t i, uint32_t first) __attribute__((always_inline)) {
@@ -267,22 +295,23 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
         KvWork x;
         x.entry = i;
         x.slot = known ? slot : 0;
-        x.length = 0;
-        if (known) {
-            const int32_t had = scalar(c.lengths)[slot];
-            x.length = had < 0 ? 0 : min(had, room);
+        const int32_t had = scalar(c.lengths)[x.slot];
+        if (whole) {
+            t = kKvTile * wave;
+            first_pages(x.slot);
         }
+        x.length = !known || had < 0 ? 0 : min(had, room);
         x.begin = 0;
         if (a.window > 0) x.begin = kv_first(x.length, a.window);
         const int32_t tile0 = x.begin & ~(kKvTile - 1);
-        x.steps = a.where ? kv_steps(x.length - tile0) : 1;
-        const KvPart part = kv_part(share_begin, share_end, first, x.steps);
+        x.steps = shares ? kv_steps(x.length - tile0) : 1;
+        const KvPart part = shares ? kv_part(share_begin, share_end, first, x.steps) : KvPart{0, 1, true};
         x.whole = part.whole;
-        x.last = !a.where || first + part.to >= share_end;
+        x.last = !shares || first + part.to >= share_end;
         x.from = tile0 + (int32_t)part.from * kKvStep;
         x.to = part.to == x.steps ? x.length : tile0 + (int32_t)part.to * kKvStep;
         if (part.from == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
-            if (a.where) {
+            if (shares) {
                 a.where[2 * (int64_t)i] = unit + i;
                 a.where[2 * (int64_t)i + 1] = (int32_t)kv_parts(w.index, w.size, first, x.steps);
             }
@@ -298,11 +327,8 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     // waves are joined: the registers are free by then, and what is left to do hides the way.
     Raw kr[2][KB], vr[2][KB];
     u32x4 q[R][KB];
-    Scalar *pages = nullptr;
     KvWork part;
     uint32_t kl = 0, vl = 0;  // the lane's place in a tile of keys and of values
-    int32_t t = 0, here[2], next[2];
-    auto page_of = [&](int32_t tok) { return tok < room ? pages[tok >> c.page_shift] : -1; };
     auto load_keys = [&](int32_t t, const int32_t *pg) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -332,39 +358,51 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
         const int lane = fresh_lane(), col = lane & 15, g = lane >> 4;
         kl = (uint32_t)SZ * kv_key_at(c, col, 8 * g);
         vl = (uint32_t)SZ * kv_value_at(c, 4 * g, 2 * col);
-        // the queries first: what is loaded after them is not waited for with them
+        if (!whole) {
+            t = part.from + kKvTile * wave;
+            first_pages(part.slot);
+        }
+        auto load_queries = [&](auto aligned) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int32_t row = row0 + 16 * r + col;
-            const bool in = row < a.group;
-            const uint16_t *src = (const uint16_t *)a.q + part.entry * a.q_stride +
-                                  (int64_t)(head * a.group + (in ? row : 0)) * D + 8 * g;
+            for (int r = 0; r < R; ++r) {
+                const int32_t row = row0 + 16 * r + col;
+                const uint16_t *src = (const uint16_t *)a.q + part.entry * a.q_stride +
+                                      (int64_t)(head * a.group + (row < a.group ? row : 0)) * D + 8 * g;
 #pragma unroll
-            for (int j = 0; j < KB; ++j) {
-                u32x4 x;
-                if (a.q_aligned) {
-                    x = *(const u32x4 *)(src + 32 * j);
-                } else {
+                for (int j = 0; j < KB; ++j) {
+                    if (decltype(aligned)::value) {
+                        q[r][j] = *(const u32x4 *)(src + 32 * j);
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = src[32 * j + 2 * e] | (uint32_t)src[32 * j + 2 * e + 1] << 16;
+                        for (int e = 0; e < 4; ++e)
+                            q[r][j][e] = src[32 * j + 2 * e] | (uint32_t)src[32 * j + 2 * e + 1] << 16;
+                    }
                 }
-                q[r][j] = in ? x : u32x4{0, 0, 0, 0};
             }
-        }
-        pages = scalar(c.table + (int64_t)part.slot * c.slot_pages);
-        t = part.from + kKvTile * wave;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            here[h] = page_of(t + 16 * h);
-            next[h] = page_of(t + kStep + 16 * h);
-        }
+        };
+        // The queries before the keys, as what is loaded after them is not waited for with
+        // them, and masked beside the loads, where what is on its way is known.
         if (t < part.to) {
+            if (a.q_aligned) load_queries(std::true_type());
+            else load_queries(std::false_type());
             load_keys(t, here);
             load_values(t, here);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                uint32_t keep = row0 + 16 * r + col < a.group ? ~0u : 0;
+                asm volatile("" : "+v"(keep));  // a mask, no branch, past which the queries might be on their way
+#pragma unroll
+                for (int j = 0; j < KB; ++j) q[r][j] &= keep;
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < KB; ++j) q[r][j] = u32x4{0, 0, 0, 0};
         }
     };
 
-    part = part_of(uniform(w.entry), first);
+    part = part_of(w.entry, first);
     start();
     for (;;) {
         const int lane = fresh_lane(), g = lane >> 4;
@@ -409,8 +447,8 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
                     for (int h = 0; h < 2; ++h) s[r][h] *= a.scale;
                 if (!full) {
                     // Kept a branch: most tiles are full, and selections and masks that do
-                    // nothing are a fifth of a tile's vector instructions (one sequence of
-                    // 611 tokens: 5.8 us, 6.0 with them).
+                    // nothing are a fifth of a tile's vector instructions (0.2 us of one
+                    // sequence of 611 tokens).
                     asm volatile("");
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {

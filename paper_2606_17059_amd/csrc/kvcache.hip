@@ -174,7 +174,7 @@ int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window,
     a->q_heads = q_heads;
     // Few sequences that cannot be long: a workgroup of many waves each, and nothing to
     // join.  That takes less than shares where a wave has a few tiles (one sequence of 611
-    // tokens, 14 heads of 64: 6.0 us, in shares 8.1; of 1,000: 7.5 and 8.3; of 2,000: 10.7
+    // tokens, 14 heads of 64: 5.4 us, in shares 8.1; of 1,000: 6.7 and 8.3; of 2,000: 10.7
     // and 8.3; 8 of 500 on 4 key heads of 256: 13.2 and 11.7), or where the workgroups fill
     // the GPU anyway (32 of 500 to 1,500 on 8 key heads of 128: 24.2, 30.0).
     const int64_t pairs = n * c->kv_heads * ((group + 15) / 16);
