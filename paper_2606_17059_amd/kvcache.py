@@ -208,7 +208,8 @@ class KVCache:
         heads, stride, io = self._rows(q, "q", n, 0)
         st = self._st(stream)
         if out is None:
-            out = self._empty(q, q.shape, stream)
+            dense = stream is None and stride == heads * self.head_dim
+            out = self._torch.empty_like(q) if dense else self._empty(q, q.shape, stream)
         elif out.dtype != q.dtype or tuple(out.shape) != tuple(q.shape) or not out.is_contiguous():
             raise ValueError("out must be a contiguous tensor of q's dtype and shape")
         elif out.device != self.device:
