@@ -548,8 +548,9 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  * is out of range are left out.  A number among those attended that is not
  * finite gives what the formula gives from a key (a score of -infinity is a
  * weight of 0, any other a NaN), and a dimension that is not finite from a
- * value.  A row all of whose weights are 0 is one without tokens.  Sums, maxima
- * and weights are kept in 32 bits: values up to 2^88 cannot overflow them.
+ * value.  A row all of whose weights are 0 is one without tokens.  Sums and
+ * maxima are kept in 32 bits (values up to 2^88 cannot overflow them), and each
+ * weight to 2^-17 of itself, however small it is beside the largest.
  * scale and scale * k_scale have to be finite.
  * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
  * out must not overlap q (from its first to its last number).

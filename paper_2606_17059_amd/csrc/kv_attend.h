@@ -78,6 +78,27 @@ struct Eight<IO, true> {
     }
 };
 
+// Eight values of the cache as bfloat16, whose exponents the weights need (see the
+// kernel).  A half number is the sum of two bfloat16 numbers, exactly: the nearest
+// leaves at most three bits.
+template <typename IO, bool E4M3>
+struct Values {
+    static constexpr bool kTwo = std::is_same_v<IO, F16> && !E4M3;
+    u32x4 first, rest;  // rest: kTwo only
+    __device__ explicit Values(typename Eight<IO, E4M3>::Raw r) {
+        if constexpr (kTwo) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = F16::low(r[i]), y = F16::high(r[i]);
+                first[i] = Bf16::pack(x, y);
+                rest[i] = Bf16::pack(x - Bf16::low(first[i]), y - Bf16::high(first[i]));
+            }
+        } else {
+            first = Eight<Bf16, E4M3>::wide(r);
+        }
+    }
+};
+
 // The larger of / the sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float rows_max(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -229,10 +250,12 @@ struct KvWork {
 // contiguous bytes too.  Keys and values go from memory to the matrix units'
 // registers without LDS.
 //
-// Weights are rounded to the value's 16-bit type twice, once for the weight and
-// once for what that left over, so that the sum's terms are good to about 2^-17
-// (bf16) or 2^-22 (f16) and the output's error is its own rounding; the second
-// MFMA costs nothing next to the loads.
+// Weights are rounded to bfloat16 twice, once for the weight and once for what that
+// left over, so that each term of the sum is good to 2^-17, however small its weight
+// (half numbers end at 2^-24 of the largest: thousands of such weights beside one large
+// one whose value is 0 are the output), and the output's error is its own rounding; the
+// second MFMA costs nothing next to the loads.  Half values are two bfloat16 numbers
+// and take a third MFMA (the rest of the value by the rest of the weight is 2^-18).
 template <typename IO, bool E4M3, int D, int R, int W>
 __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_kernel(KvAttend a) {
     using Raw = typename Eight<IO, E4M3>::Raw;
@@ -489,8 +512,8 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
                     l[r] += sum;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        hi[r][i] = IO::pack(x[2 * i], x[2 * i + 1]);
-                        lo[r][i] = IO::pack(x[2 * i] - IO::low(hi[r][i]), x[2 * i + 1] - IO::high(hi[r][i]));
+                        hi[r][i] = Bf16::pack(x[2 * i], x[2 * i + 1]);
+                        lo[r][i] = Bf16::pack(x[2 * i] - Bf16::low(hi[r][i]), x[2 * i + 1] - Bf16::high(hi[r][i]));
                     }
                 }
             }
@@ -511,14 +534,17 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
             }
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
-                const u32x4 v0 = Eight<IO, E4M3>::wide(vr[0][j]), v1 = Eight<IO, E4M3>::wide(vr[1][j]);
+                const Values<IO, E4M3> v0(vr[0][j]), v1(vr[1][j]);
+                auto pair = [](u32x4 a, u32x4 b, int e) { return u32x4{a[2 * e], a[2 * e + 1], b[2 * e], b[2 * e + 1]}; };
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const u32x4 vv{v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1]};
+                    const u32x4 vv = pair(v0.first, v1.first, e);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        o[r][j][e] = IO::mfma(vv, hi[r], o[r][j][e]);
-                        o[r][j][e] = IO::mfma(vv, lo[r], o[r][j][e]);
+                        o[r][j][e] = Bf16::mfma(vv, hi[r], o[r][j][e]);
+                        o[r][j][e] = Bf16::mfma(vv, lo[r], o[r][j][e]);
+                        if constexpr (Values<IO, E4M3>::kTwo)
+                            o[r][j][e] = Bf16::mfma(pair(v0.rest, v1.rest, e), hi[r], o[r][j][e]);
                     }
                 }
             }

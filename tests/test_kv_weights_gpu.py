@@ -1,0 +1,75 @@
+"""Attention where one token's weight is far above the others' and its value is 0, as with an attention sink: the
+output is the sum of many small weights, each of which has to be good by itself."""
+import math
+
+import pytest
+
+from gpu_util import announce, device
+from test_kv_gpu import _cache, _check_attend, _ints, _offsets, _types
+
+pytestmark = pytest.mark.gpu
+
+
+def _sink_case(kind, io, dim, lengths, gap, at, slot_pages=None, size=1.0):
+    """Sequences of equal scores but one, 2^gap times as heavy, at token `at` of each.  Scores are products of powers
+    of two by the scale, so that they are exact; values of the others lie in [size / 2, 3 size / 2]."""
+    import torch
+    announce(f"attend {kind} {io} dim {dim} lengths {lengths} gap {gap} at {at}")
+    heads, total = 2, sum(lengths)
+    c = _cache(1, heads, dim, 16, sum(-(-n // 16) for n in lengths) + 1, len(lengths),
+               slot_pages or max(-(-n // 16) for n in lengths), kind,
+               **(dict(k_scale=0.5, v_scale=max(1.0, size / 256)) if kind == "e4m3" else {}))
+    place = c.extend(_ints(range(len(lengths))), _offsets(lengths), total)
+    g = torch.Generator(device=device()).manual_seed(dim)
+    k = torch.zeros((total, heads, dim), device=device())
+    v = torch.empty((total, heads, dim), device=device()).uniform_(0.5 * size, 1.5 * size, generator=g)
+    for i, n in enumerate(lengths):
+        row = sum(lengths[:i]) + at % n
+        k[row, :, dim - 1] = 16.0
+        v[row] = 0.0
+    c.write(0, place, k.to(_types()[io]), v.to(_types()[io]))
+    q = torch.zeros((len(lengths), 2 * heads, dim), dtype=_types()[io], device=device())
+    q[:, :, dim - 1] = 1.0
+    scale = gap * math.log(2.0) / 16.0
+    lse = torch.empty((len(lengths), 2 * heads), device=device())
+    out = c.attend(0, _ints(range(len(lengths))), q, scale, lse=lse)
+    # the library's scale is a float32 number
+    _check_attend(c, 0, list(range(len(lengths))), q, scale, 0, out, lse)
+    c.check()
+    return out
+
+
+@pytest.mark.parametrize("kind,io", [("fp16", "fp16"), ("e4m3", "fp16"), ("e4m3", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("gap", [6.0, 18.5, 20.4, 23.5, 25.2])
+def test_attend_one_heavy_token_without_value(kind, io, dim, gap):
+    """A workgroup a sequence, and shares with their joins; the heavy token first and last."""
+    for at in (0, -1):
+        _sink_case(kind, io, dim, [32, 611, 5], gap, at)
+        _sink_case(kind, io, dim, [2816, 40], gap, at, slot_pages=400)
+
+
+@pytest.mark.parametrize("kind,io", [("fp16", "fp16"), ("e4m3", "fp16")])
+@pytest.mark.parametrize("gap", [32.0, 38.0])
+def test_attend_small_weights_of_large_values(kind, io, gap):
+    """Weights far below the smallest half number whose products with the values are not."""
+    out = _sink_case(kind, io, 64, [611], gap, 0, size=24576.0)
+    assert (out > 0).all()
+    _sink_case(kind, io, 128, [2816], gap, 0, slot_pages=400, size=24576.0)
+
+
+def test_attend_half_values_in_full():
+    """Every finite half value, one a sequence of equal tokens: the output is the value, bit for bit.  (Weights are 1:
+    the value's two parts and the division by their number are exact.)"""
+    import torch
+    announce("attend to every half value")
+    dim, heads, n = 64, 8, 128
+    c = _cache(1, heads, dim, 16, n, n, 1, "fp16")
+    bits = torch.arange(65536, device=device()).to(torch.int16).view(torch.float16).view(n, heads, dim)
+    x = torch.where(bits.isfinite(), bits, torch.zeros_like(bits))
+    place = c.extend(_ints(range(n)), _offsets([2] * n), 2 * n)
+    rows = x.repeat_interleave(2, 0)
+    c.write(0, place, torch.zeros_like(rows), rows)
+    out = c.attend(0, _ints(range(n)), torch.ones((n, heads, dim), dtype=torch.float16, device=device()), 1.0)
+    assert torch.equal(out + 0.0, x + 0.0)  # -0 is 0
+    c.check()
