@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <utility>
 
 #include "kv_launch.h"
 #include "kv_pages.h"
@@ -50,6 +51,26 @@ constexpr int64_t kMostRows = INT32_MAX;
 
 int element_bytes(const pr_kv *c) { return c->dtype == PR_KV_E4M3 ? 1 : 2; }
 
+// Whether of the blocks of `page` elements at i * a + j * b (0 <= i < na, 0 <= j < nb)
+// two overlap.
+bool overlap(int64_t page, int64_t a, int64_t na, int64_t b, int64_t nb) {
+    if ((na > 1 && a < page) || (nb > 1 && b < page)) return true;
+    if (na == 1 || nb == 1) return false;
+    if (a > b) {
+        std::swap(a, b);
+        std::swap(na, nb);
+    }
+    // Each row of the smaller stride ends before the next begins, but for orders that
+    // nothing has; there, the blocks next to each row's first are looked at.
+    const __int128 row = (__int128)a * (na - 1) + page;
+    for (int64_t j = 1; j < nb && (__int128)j * b < row; ++j) {
+        const __int128 at = (__int128)j * b;
+        const int64_t i = (int64_t)(at / a), past = (int64_t)(at % a);
+        if ((i < na && past < page) || (i + 1 < na && a - past < page)) return true;
+    }
+    return false;
+}
+
 // nullptr if c describes a cache, else what is wrong with it.
 const char *wrong(const pr_kv *c) {
     if (!c) return "pr_kv is NULL";
@@ -70,8 +91,13 @@ const char *wrong(const pr_kv *c) {
     if (c->kv_heads > (1 << 20) || page * 2 > INT32_MAX) return "a page must be smaller than 2^31 bytes";
     for (const int64_t s : {c->k_layer, c->k_page, c->v_layer, c->v_page})
         if (s < 0 || s % unit) return "strides must be non-negative multiples of 16 bytes";
-    if ((c->num_pages > 1 && (c->k_page < page || c->v_page < page)) ||
-        (c->layers > 1 && (c->k_layer < page || c->v_layer < page)))
+    auto extent = [&](int64_t layer, int64_t each) {
+        return (__int128)layer * (c->layers - 1) + (__int128)each * (c->num_pages - 1);
+    };
+    if (std::max(extent(c->k_layer, c->k_page), extent(c->v_layer, c->v_page)) > ((int64_t)1 << 60))
+        return "strides are too large";
+    if (overlap(page, c->k_layer, c->layers, c->k_page, c->num_pages) ||
+        overlap(page, c->v_layer, c->layers, c->v_page, c->num_pages))
         return "pages must not overlap";
     if (c->dtype == PR_KV_E4M3) {
         if (!(std::isfinite(c->k_scale) && c->k_scale > 0 && std::isfinite(c->v_scale) && c->v_scale > 0))
