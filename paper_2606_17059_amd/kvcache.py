@@ -33,6 +33,8 @@ class KVCache:
 
     The tensors are the caller's and stay as they are; `create` makes an empty
     cache.  Calls run on the current stream of the cache's device, or on `stream`.
+    They have no derivatives: floating-point tensors that require gradients (but
+    under torch.no_grad()) or carry a forward-mode tangent are refused.
     """
 
     def __init__(self, k, v, table, lengths, refs, free, k_scale: float = 1.0, v_scale: float = 1.0, skipped=None):
@@ -45,6 +47,8 @@ class KVCache:
                 raise TypeError("k and v must both be bfloat16, float16 or float8_e4m3fn")
             if t.dim() != 6 or t.numel() == 0 or not t[0, 0].is_contiguous():
                 raise ValueError(f"{name} must have 6 dimensions, none empty, the last four contiguous")
+            if t.requires_grad:
+                raise ValueError(f"{name} must not require gradients: the calls have none")
         layers, pages, heads, eights, tokens, eight = k.shape
         dim = 8 * eights
         if eight != 8 or tuple(v.shape) != (layers, pages, heads, tokens // 4, dim, 4) or tokens % 4:
@@ -75,6 +79,7 @@ class KVCache:
             free.data_ptr() or None, skipped.data_ptr())
         self._ref = ctypes.byref(self._desc)
         self._torch, self._index, self._int32, self._int64 = torch, k.device.index, torch.int32, torch.int64
+        self._forward_ad = torch.autograd.forward_ad
         # types that rows of new tokens and queries may have
         self._io = {torch.bfloat16: PR_KV_BF16, torch.float16: PR_KV_F16} if k.dtype.itemsize == 1 else \
             {k.dtype: codes[k.dtype]}
@@ -161,7 +166,16 @@ class KVCache:
             raise ValueError(f"rows of {name} must be contiguous")
         if io < 0:
             raise TypeError(f"{name} must be of the cache's type, or bfloat16 or float16 for a float8 cache")
+        if t.requires_grad or self._forward_ad._current_level >= 0:  # no tensor has a tangent outside a level
+            self._no_derivative(t, name)
         return shape[1], stride[0], io
+
+    def _no_derivative(self, t, name) -> None:
+        if t.requires_grad and self._torch.is_grad_enabled():
+            raise ValueError(f"{name} requires gradients, which this call does not give: detach it, or call under "
+                             "torch.no_grad()")
+        if self._forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} carries a tangent, which this call does not follow")
 
     # ---- calls --------------------------------------------------------------------
     def init(self, stream=None) -> None:
@@ -214,10 +228,13 @@ class KVCache:
             raise ValueError("out must be a contiguous tensor of q's dtype and shape")
         elif out.device != self.device:
             raise ValueError("out must be on the cache's device")
+        else:
+            self._no_derivative(out, "out")
         if lse is not None:
             _dev(lse, self._torch.float32, "lse")
             if tuple(lse.shape) != (n, heads) or lse.device != self.device:
                 raise ValueError("lse must be [n, heads] on the cache's device")
+            self._no_derivative(lse, "lse")
         work, at, size = self._work(PR_KV_WORK_ATTEND, n, heads, stream)
         s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, stride,
                                    heads, io, self._scale if scale is None else scale, min(window, 0x7fffffff),

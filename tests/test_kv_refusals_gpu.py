@@ -1,0 +1,50 @@
+"""What the KV cache's binding refuses, and what it must go on taking."""
+import pytest
+
+from gpu_util import announce, device
+from test_kv_gpu import _cache, _fill, _ints, _offsets
+
+pytestmark = pytest.mark.gpu
+
+
+def _ready():
+    import torch
+    c = _cache(2)
+    _fill(c, [5, 20])
+    q = torch.randn((2, 4, 64), device=device()).bfloat16()
+    return c, _ints([0, 1]), q
+
+
+def test_gradients_are_refused_not_dropped():
+    import torch
+    import torch.autograd.forward_ad as forward_ad
+    from paper_2606_17059_amd import KVCache
+    announce("tensors that require gradients")
+    c, slots, q = _ready()
+    want = c.attend(0, slots, q)
+    place = c.extend(slots, _offsets([1, 1]), 2)
+    rows = q[:, :2].contiguous()
+    leaf, lse = q.clone().requires_grad_(), torch.zeros((2, 4), device=device())
+    for f in (lambda: c.attend(0, slots, leaf), lambda: c.attend(0, slots, leaf * 2),
+              lambda: c.attend(0, slots, q, out=torch.zeros_like(q).requires_grad_()),
+              lambda: c.attend(0, slots, q, lse=lse.clone().requires_grad_()),
+              lambda: c.write(0, place, rows.clone().requires_grad_(), rows),
+              lambda: c.write(0, place, rows, rows.clone().requires_grad_()),
+              lambda: KVCache(c.k.clone().requires_grad_(), c.v, c.table, c.lengths, c.refs, c.free),
+              lambda: KVCache(c.k, c.v.clone().requires_grad_(), c.table, c.lengths, c.refs, c.free)):
+        with pytest.raises(ValueError, match="gradients"):
+            f()
+    with torch.no_grad(), forward_ad.dual_level():
+        dual = forward_ad.make_dual(rows, rows)
+        for f in (lambda: c.attend(0, slots, forward_ad.make_dual(q, q)), lambda: c.write(0, place, dual, rows),
+                  lambda: c.write(0, place, rows, dual)):
+            with pytest.raises(ValueError, match="tangent"):
+                f()
+        c.write(0, place, rows, rows)  # others go on
+    c.trim(slots, _ints([5, 20]))
+    for ask in (torch.no_grad, torch.inference_mode):
+        with ask():
+            got = c.attend(0, slots, leaf)
+            assert torch.equal(got, want) and not got.requires_grad
+    assert torch.equal(c.attend(0, slots, leaf.detach()), want)
+    c.check()
