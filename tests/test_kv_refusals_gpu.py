@@ -48,3 +48,27 @@ def test_gradients_are_refused_not_dropped():
             assert torch.equal(got, want) and not got.requires_grad
     assert torch.equal(c.attend(0, slots, leaf.detach()), want)
     c.check()
+
+
+@pytest.mark.parametrize("layer", [-1, 2, 2 ** 31, -2 ** 31, 2 ** 32, 2 ** 32 + 1, -2 ** 32, 2 ** 64, -2 ** 64])
+def test_layers_past_32_bits_are_no_layers(layer):
+    """A layer's number is 32 bits wide in the C call: what does not fit must not become another layer."""
+    announce(f"layer {layer}")
+    c, slots, q = _ready()
+    place = c.extend(slots, _offsets([1, 1]), 2)
+    rows = q[:, :2].contiguous()
+    k, v = c.k.clone(), c.v.clone()
+    with pytest.raises(RuntimeError, match="layer"):
+        c.attend(layer, slots, q)
+    with pytest.raises(RuntimeError, match="layer"):
+        c.write(layer, place, rows, rows)
+    import torch
+    assert torch.equal(c.k.view(torch.int16), k.view(torch.int16)) and torch.equal(c.v.view(torch.int16), v.view(torch.int16))
+
+
+@pytest.mark.parametrize("window", [-1, -2 ** 31, -2 ** 31 - 1, -2 ** 32, -2 ** 32 + 7, -2 ** 64])
+def test_negative_windows_past_32_bits_are_negative(window):
+    announce(f"window {window}")
+    c, slots, q = _ready()
+    with pytest.raises(RuntimeError, match="window"):
+        c.attend(0, slots, q, window=window)
