@@ -348,37 +348,55 @@ __global__ void __launch_bounds__(256) kv_extend_place_kernel(KvExtend x, uint32
 }
 
 // ---- rows ------------------------------------------------------------------------
+// A scale without its power of two, so that quotients by it neither overflow nor lose
+// bits: number / scale is (number * shift) / unit.
+struct KvUnit {
+    float shift, unit, over;  // over: 1 / unit
+};
+
 struct KvRows {
     KvView c;
     const int32_t *place;
     const void *k, *v;
     int64_t k_stride, v_stride, rows, layer;
     bool aligned;  // rows may be read 16 bytes at a time
+    KvUnit k_unit, v_unit;
 };
 
 // Conversion of eight 16-bit numbers of a row to what the cache holds.
 struct KvSame {
     using T = uint16_t;
-    __device__ static void put(const uint16_t *in, float, T *out) {
+    __device__ static void put(const uint16_t *in, const KvUnit &, T *out) {
         for (int i = 0; i < 8; ++i) out[i] = in[i];
     }
 };
-// Nearest e4m3 of number / scale.  The conversion instruction rounds to nearest,
-// ties to even; what lies past the range is held at its end first, NaN kept.
+// Nearest e4m3 of number / scale.  The conversion instruction rounds to nearest, ties
+// to even.  The quotient's own rounding must not make a tie of what is none (1.25 by the
+// float next to 1.25 / 19 is not 19, which lies between 18 and 20): an inexact one is made
+// odd, towards the exact one, and so keeps its side of every tie.  A product with the
+// reciprocal, corrected once by what it leaves, does for the division (34,000 rows of 8
+// heads of 128: 56 us; with divisions 66, and 52 without the care for ties).
 template <bool BF16>
 struct KvE4m3 {
     using T = uint8_t;
-    __device__ static float one(uint16_t b, float scale) {
+    __device__ static float quotient(uint16_t b, const KvUnit &u) {
         float x;
         if (BF16) x = __uint_as_float((uint32_t)b << 16);
         else x = (float)__builtin_bit_cast(_Float16, b);
-        x = x / scale;
-        return x > 448.f ? 448.f : (x < -448.f ? -448.f : x);
+        const float top = 456.f * u.unit;  // between 448, the last, and what would round past it
+        const float in = __builtin_amdgcn_fmed3f(x * u.shift, -top, top);
+        float y = in * u.over;
+        y = __builtin_fmaf(__builtin_fmaf(-y, u.unit, in), u.over, y);  // the nearest, or beside it next to a tie of floats
+        const uint32_t left = __float_as_uint(__builtin_fmaf(-y, u.unit, in)), bits = __float_as_uint(y);
+        const uint32_t inexact = min(left << 1, 1u);
+        // towards 0, and odd if inexact
+        y = __uint_as_float((bits - ((bits ^ left) >> 31 & inexact)) | inexact);
+        return x != x ? x : y;
     }
-    __device__ static void put(const uint16_t *in, float scale, T *out) {
+    __device__ static void put(const uint16_t *in, const KvUnit &u, T *out) {
         for (int i = 0; i < 8; i += 4) {
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(one(in[i], scale), one(in[i + 1], scale), 0, false);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(one(in[i + 2], scale), one(in[i + 3], scale), w, true);
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(in[i], u), quotient(in[i + 1], u), 0, false);
+            w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(in[i + 2], u), quotient(in[i + 3], u), w, true);
             for (int e = 0; e < 4; ++e) out[i + e] = (uint8_t)((uint32_t)w >> (8 * e));
         }
     }
@@ -456,9 +474,9 @@ __global__ void __launch_bounds__(256) kv_write_kernel(KvRows x) {
         } else {
             kv_load8(vrow, x.aligned, val);
         }
-        P::put(key, c.k_scale, one.e);
+        P::put(key, x.k_unit, one.e);
         *(V8 *)((T *)c.k + x.layer * c.k_layer + page * c.k_page + kv_head_base(c, head) + kv_key_at(c, t, d)) = one.v;
-        P::put(val, c.v_scale, one.e);
+        P::put(val, x.v_unit, one.e);
         T *dst = (T *)c.v + x.layer * c.v_layer + page * c.v_page + kv_head_base(c, head) + kv_value_at(c, t & ~3, d);
         if (whole) {
             *(V8 *)(dst + 4 * two) = one.v;

@@ -329,7 +329,12 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
     DeviceScope ds(c->device);
     if (!ds.ok()) return fail(PR_EDEVICE, "cannot select the cache's device");
     const bool aligned = !((((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) || (rows > 1 && (k_stride | v_stride) & 7));
-    const pr::KvRows x{view(c), place, k_rows, v_rows, k_stride, v_stride, rows, layer, aligned};
+    auto unit = [](float scale) {
+        const int e = std::min(std::max(std::ilogb(scale), -126), 126);  // both powers are floats
+        const float u = std::ldexp(scale, -e);
+        return pr::KvUnit{std::ldexp(1.f, -e), u, 1.f / u};
+    };
+    const pr::KvRows x{view(c), place, k_rows, v_rows, k_stride, v_stride, rows, layer, aligned, unit(c->k_scale), unit(c->v_scale)};
     hipStream_t st = (hipStream_t)hip_stream;
     const unsigned grid = (blocks((rows + 7) / 8 * ((width + 63) / 64) * 64, kMostGrid - 7) + 7) / 8 * 8;
     if (c->dtype != PR_KV_E4M3) pr::kv_write_kernel<pr::KvSame><<<grid, 256, 0, st>>>(x);
