@@ -614,7 +614,9 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
                     const int64_t to_row = (int64_t)done.entry * a.q_heads + at;
                     if (a.lse && j == 0 && g == 0)
                         a.lse[to_row] = (most + log2f(sum)) * 0.6931471805599453f;
-                    const float unit_v = sum == 0.f ? 0.f : c.v_scale / sum;  // 0: no token counts
+                    const bool none = sum == 0.f;  // no token counts, whatever 0 times its value is
+                    const float unit_v = none ? 0.f : c.v_scale / sum;
+                    if (none) u = v = f32x4{0, 0, 0, 0};
                     *(u32x4 *)((uint32_t *)a.out + (to_row * D + 32 * j + 8 * g) / 2) =
                         u32x4{IO::pack(u[0] * unit_v, v[0] * unit_v), IO::pack(u[1] * unit_v, v[1] * unit_v),
                               IO::pack(u[2] * unit_v, v[2] * unit_v), IO::pack(u[3] * unit_v, v[3] * unit_v)};
@@ -707,7 +709,9 @@ __global__ void __launch_bounds__(kv_join_threads(D, MANY)) kv_join_kernel(KvAtt
     if (!in) return;
     const int64_t to_row = entry * a.q_heads + row;
     if (a.lse && col == 0) a.lse[to_row] = (m + log2f(l)) * 0.6931471805599453f;
-    const float unit_v = l == 0.f ? 0.f : a.c.v_scale / l;
+    const bool none = l == 0.f;
+    const float unit_v = none ? 0.f : a.c.v_scale / l;
+    if (none) o = f32x4{0, 0, 0, 0};
     *(u32x2 *)((uint32_t *)a.out + (to_row * D + 4 * col) / 2) =
         u32x2{IO::pack(o[0] * unit_v, o[1] * unit_v), IO::pack(o[2] * unit_v, o[3] * unit_v)};
 }

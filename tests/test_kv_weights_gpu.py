@@ -73,3 +73,26 @@ def test_attend_half_values_in_full():
     out = c.attend(0, _ints(range(n)), torch.ones((n, heads, dim), dtype=torch.float16, device=device()), 1.0)
     assert torch.equal(out + 0.0, x + 0.0)  # -0 is 0
     c.check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_attend_no_weight_beside_values_that_are_not_finite(kind):
+    """Scores that are all -infinity are a row without tokens, whatever the values hold."""
+    import torch
+    announce(f"attend without weights, {kind}, values not finite")
+    for lengths, slot_pages in (([40, 3], 3), ([3000, 5], 400)):  # a workgroup a sequence; shares and their join
+        c = _cache(1, 1, 64, 16, sum(-(-n // 16) for n in lengths), 2, slot_pages, kind)
+        place = c.extend(_ints([0, 1]), _offsets(lengths), sum(lengths))
+        k = torch.zeros((sum(lengths), 1, 64), dtype=_types()[kind], device=device())
+        v = torch.ones_like(k)
+        k[:, :, 3] = -math.inf
+        v[1::3, :, 5], v[::7, :, 9], v[2::5, :, 60] = math.inf, math.nan, -math.inf
+        c.write(0, place, k, v)
+        q = torch.zeros((2, 2, 64), dtype=k.dtype, device=device())
+        q[:, :, 3] = 1.0
+        lse = torch.zeros((2, 2), device=device())
+        out = c.attend(0, _ints([0, 1]), q, 1.0, lse=lse)
+        assert (out == 0).all() and (lse == -math.inf).all(), lengths
+        c.k[:, :, :, 0, :, 3] = 0  # all weights the same: each dimension is what its values make it
+        out = c.attend(0, _ints([0, 1]), q, 1.0, lse=lse)
+        assert not out[0, :, [5, 9, 60]].isfinite().any() and (out[:, :, [0, 4, 6, 63]] == 1).all()
