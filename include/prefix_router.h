@@ -597,7 +597,9 @@ pr_status pr_kv_compact(const pr_kv *c, int32_t *moved, void *workspace, int64_t
 
 /* Wait for the stream and report batch entries that calls skipped since the
  * last check: PR_OK if none, else PR_EINVAL with the count in the message (and
- * resets the count).  Not for streams under capture (PR_ESTATE). */
+ * takes them from the count; what attentions on other streams add meanwhile is
+ * the next check's).  Checks of one cache must not overlap.  Not for streams
+ * under capture (PR_ESTATE). */
 pr_status pr_kv_check(const pr_kv *c, void *hip_stream);
 
 #ifdef __cplusplus

@@ -92,6 +92,11 @@ __global__ void __launch_bounds__(256) kv_init_kernel(KvView c) {
     if (first == 0) *c.skipped = 0;
 }
 
+// Takes entries that were reported from the count.
+__global__ void __launch_bounds__(1) kv_reported_kernel(unsigned long long *skipped, unsigned long long reported) {
+    atomicAdd(skipped, 0 - reported);
+}
+
 // What kv_extend_plan_kernel decides about an entry.
 struct KvGrant {
     int32_t start;   // tokens the sequence held

@@ -471,8 +471,9 @@ pr_status pr_kv_check(const pr_kv *c, void *hip_stream) {
         hipStreamSynchronize(st) != hipSuccess)
         return fail(PR_EDEVICE, "reading the skipped entries failed");
     if (skipped == 0) return ok();
-    if (hipMemsetAsync(c->skipped, 0, sizeof skipped, st) != hipSuccess ||
-        hipStreamSynchronize(st) != hipSuccess)
+    // what attentions on other streams count meanwhile stays for the next check
+    pr::kv_reported_kernel<<<1, 1, 0, st>>>((unsigned long long *)c->skipped, (unsigned long long)skipped);
+    if (hipGetLastError() != hipSuccess || hipStreamSynchronize(st) != hipSuccess)
         return fail(PR_EDEVICE, "resetting the skipped entries failed");
     char msg[96];
     snprintf(msg, sizeof msg, "%lld batch entries were skipped", (long long)skipped);

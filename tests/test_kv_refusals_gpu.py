@@ -72,3 +72,39 @@ def test_negative_windows_past_32_bits_are_negative(window):
     c, slots, q = _ready()
     with pytest.raises(RuntimeError, match="window"):
         c.attend(0, slots, q, window=window)
+
+
+def test_checks_lose_no_entries_that_other_streams_count():
+    """Attentions of unknown slots go on while another stream's checks report and reset the count: all are reported."""
+    import re
+    import torch
+    from paper_2606_17059_amd import RouterError
+    announce("checks beside attentions on another stream")
+    c, _, q = _ready()
+    bad = _ints([99, -7])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    total = 0
+
+    def check():
+        try:
+            c.check()
+        except RouterError as e:
+            return int(re.search(r"(\d+) batch entries", str(e))[1])
+        return 0
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(100):
+            c.attend(0, bad, q)
+    for _ in range(10):
+        with torch.cuda.stream(side):
+            for _ in range(5):
+                graph.replay()
+            done = torch.cuda.Event()
+            done.record()
+        while not done.query():
+            total += check()
+    torch.cuda.synchronize()
+    total += check()
+    assert total == 10 * 5 * 100 * 2 and int(c.skipped) == 0
