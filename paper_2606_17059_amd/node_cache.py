@@ -79,7 +79,7 @@ class NodeCache:
         """Put a sequence of one token or more into the cache: a fork of its longest cached prefix, with room for
         the rest.  Where no slot or too few pages are free, the least recently used sequences are given up.  Raises
         ValueError if the sequence does not fit an empty cache."""
-        t = np.ascontiguousarray(tokens, dtype=np.int32)
+        t = np.array(tokens, dtype=np.int32)  # kept: not the caller's, who may fill it anew
         c, T = self.cache, self.cache.page_tokens
         pages = -(-len(t) // T)
         if len(t) == 0 or pages > min(c.table.shape[1], c.pages):
