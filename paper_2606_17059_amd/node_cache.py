@@ -33,11 +33,14 @@ class NodeCache:
     """forest: the node's; local: its own tree's peer id there; cache: an empty KVCache with at most PR_MAX_PEERS
     slots.  Calls are host-synchronous and run on the current stream."""
 
+    SPARE = 1 << 16  # nodes and label tokens out of use that the index may have beside as many as it had in use
+
     def __init__(self, forest: Forest, local: int, cache: KVCache):
         self.forest, self.local, self.cache = forest, int(local), cache
         self.slots = cache.lengths.shape[0]
         self.index = Forest(self.slots)
         self.tokens: Dict[int, np.ndarray] = {}  # per slot in use, least recently used first
+        self._least = 0  # size of the index after its last compaction
 
     def _ints(self, x):
         import torch
@@ -56,6 +59,15 @@ class NodeCache:
         self.tokens.pop(slot, None)
         if len(tokens):
             self.tokens[slot] = tokens
+        # a slot's next sequence leaves its last one's nodes and labels behind (3,000 admissions to six slots: 453,036
+        # nodes of which 12 were in use)
+        if self._size() > 2 * self._least + self.SPARE:
+            self.index.compact()
+            self._least = self._size()
+
+    def _size(self) -> int:
+        info = self.index.info()
+        return info["num_nodes"] + info["pool_tokens"]
 
     def drop(self, slots) -> None:
         """Give up the sequences of these slots (evictKVCache)."""

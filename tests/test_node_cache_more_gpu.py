@@ -39,3 +39,26 @@ def test_a_callers_array_is_not_kept():
     assert node.lookup(buf) == (-1, 0)
     node.close()
     f.close()
+
+
+def test_the_index_stays_as_small_as_what_is_cached():
+    """Thousands of sequences through a few slots: the index holds the last ones, not all there were, and finds them."""
+    announce("1,500 admissions to six slots")
+    f, node = _node()
+    rng = np.random.default_rng(2)
+    head = rng.integers(0, 1000, 40).astype(np.int32)
+    most = 0
+    for i in range(1500):
+        t = np.concatenate([head, rng.integers(0, 1000, 60).astype(np.int32)])
+        a = node.admit(t)
+        assert a.cached >= 40 * (i > 0)
+        info = node.index.info()
+        most = max(most, info["num_nodes"] + info["pool_tokens"])
+        if i % 100 == 0:
+            for s, x in node.tokens.items():
+                assert node.lookup(x)[1] == len(x)
+    # twice what six sequences of 100 tokens need, the spare room, and what one admission adds
+    assert most < 2 * 6 * 200 + node.SPARE + 4096
+    node.cache.check()
+    node.close()
+    f.close()
