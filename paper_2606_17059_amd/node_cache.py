@@ -30,8 +30,9 @@ class Admission(NamedTuple):
 
 
 class NodeCache:
-    """forest: the node's; local: its own tree's peer id there; cache: an empty KVCache with at most PR_MAX_PEERS
-    slots.  Calls are host-synchronous and run on the current stream."""
+    """forest: the node's, on the cache's device; local: its own tree's peer id there; cache: an empty KVCache with at
+    most PR_MAX_PEERS slots.  Calls are host-synchronous and run on the current stream of that device, whichever device
+    is current.  The rows of an admission have to be written before the next call, which may share or copy them."""
 
     SPARE = 1 << 16  # nodes and label tokens out of use that the index may have beside as many as it had in use
 
@@ -55,14 +56,17 @@ class NodeCache:
 
     def _set(self, slot: int, tokens: np.ndarray) -> None:
         """The slot's sequence, in the index and here (an empty one: the slot is free)."""
-        self.index.load_snapshot_device(slot, *self._csr([tokens] if len(tokens) else []))
+        import torch
+        with torch.cuda.device(self.cache.device):  # a forest is of the device that is current at its first call
+            self.index.load_snapshot_device(slot, *self._csr([tokens] if len(tokens) else []))
         self.tokens.pop(slot, None)
         if len(tokens):
             self.tokens[slot] = tokens
         # a slot's next sequence leaves its last one's nodes and labels behind (3,000 admissions to six slots: 453,036
         # nodes of which 12 were in use)
         if self._size() > 2 * self._least + self.SPARE:
-            self.index.compact()
+            with torch.cuda.device(self.cache.device):
+                self.index.compact()
             self._least = self._size()
 
     def _size(self) -> int:
