@@ -48,8 +48,6 @@ constexpr int kv_resident(bool e4m3, int head_dim, int rows, int waves) {
     return waves == kKvWaves ? many : waves / 4;
 }
 
-constexpr int kKvWideWaves = 8;  // waves of a workgroup that takes a whole short sequence
-
 constexpr int kKvJoinMany = 1024;  // rows from which a joining workgroup takes several
 
 hipError_t kv_launch_bf16(const KvAttend &a, bool e4m3, hipStream_t st);

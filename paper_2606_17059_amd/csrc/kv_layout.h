@@ -55,6 +55,7 @@ constexpr int32_t kKvMostTokens = 1 << 30;  // of a sequence
 constexpr int kKvTile = 32;        // tokens a wave takes at a time
 constexpr int kKvWaves = 4;        // waves of a workgroup that takes a share of a batch
 constexpr int kKvStep = kKvTile * kKvWaves;
+constexpr int kKvWideWaves = 8;    // waves of a workgroup that takes a whole short sequence
 
 // First token attended, rounded down to a tile, and the tiles' tokens from there.
 PR_KV_FN int32_t kv_first(int32_t length, int32_t window) {
