@@ -125,16 +125,18 @@ __device__ __forceinline__ Scalar *scalar(const int32_t *p) { return (Scalar *)(
 struct KvShare {
     uint32_t begin, end, size, first, index;
     int32_t entry;
+    uint32_t number;  // see kv_part_at
 };
 __device__ __forceinline__ KvShare kv_share_of(uint32_t u, uint32_t size, uint32_t steps, const KvSplit &s) {
-    KvShare r{kv_share_begin(u, size, steps, s), steps, size, 0, u, -1};
+    KvShare r{kv_share_begin(u, size, steps, s), steps, size, 0, u, -1, u};
     r.end = min(r.begin + size, steps);
     return r;
 }
-// Share k of an entry's own.
-__device__ __forceinline__ KvShare kv_own_share(int32_t entry, uint32_t steps, uint32_t shares, uint32_t k) {
+// Share k of an entry's own, `split` the shares of the entries before it that have several.
+__device__ __forceinline__ KvShare kv_own_share(int32_t entry, uint32_t steps, uint32_t shares, uint32_t k,
+                                                uint32_t split) {
     const uint32_t size = kv_even(steps, shares);
-    return KvShare{k * size, min((k + 1) * size, steps), size, 0, 0, entry};
+    return KvShare{k * size, min((k + 1) * size, steps), size, 0, 0, entry, split + k};
 }
 
 // Share u of a batch of at most E * 64 entries, found by every wave for itself from
@@ -162,6 +164,14 @@ __device__ inline KvShare kv_find_share(const KvAttend &a, uint32_t u) {
             upto[e] = total + (uint32_t)lanes_upto((int32_t)mine[e]);
             total = (uint32_t)__builtin_amdgcn_readlane((int)upto[e], 63);
         }
+    };
+    // lane `i` of the batch's
+    auto of = [&](const uint32_t *x, int i) {
+        uint32_t r = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e == i >> 6) r = (uint32_t)__builtin_amdgcn_readlane((int)x[e], i & 63);
+        return r;
     };
     // the entry in whose part of the sums v lies
     int entry = -1;
@@ -195,17 +205,20 @@ __device__ inline KvShare kv_find_share(const KvAttend &a, uint32_t u) {
     }
     add();
     find(u);
-    if (entry < 0) return KvShare{0, 0, 1, 0, 0, -1};
-    uint32_t own = 0;
+    if (entry < 0) return KvShare{0, 0, 1, 0, 0, -1, 0};
+    uint32_t split = 0;
+    if (its > 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (e == entry >> 6) own = (uint32_t)__builtin_amdgcn_readlane((int)steps[e], entry & 63);
-    return kv_own_share(entry, own, its, u - before);
+        for (int e = 0; e < E; ++e) mine[e] = mine[e] > 1 ? mine[e] : 0;
+        add();
+        split = of(upto, entry) - its;
+    }
+    return kv_own_share(entry, of(steps, entry), its, u - before, split);
 }
 
 // The same from a plan (kv_plan_kernel) for larger batches: a.plan[i] is the steps
 // before entry i, a.plan[n] all of them; where shares keep to sequences, a.plan[n + 1 + i]
-// is the shares before entry i.
+// is the shares before entry i, a.plan[2 n + 2 + i] those of entries that have several.
 __device__ inline KvShare kv_planned_share(const KvAttend &a, uint32_t u) {
     Scalar *before = scalar(a.plan);
     const uint32_t total = (uint32_t)before[a.n];
@@ -222,7 +235,7 @@ __device__ inline KvShare kv_planned_share(const KvAttend &a, uint32_t u) {
     }
     if (keeps)
         return kv_own_share(lo, (uint32_t)before[lo + 1] - (uint32_t)before[lo], (uint32_t)sums[lo + 1] - (uint32_t)sums[lo],
-                            u - (uint32_t)sums[lo]);
+                            u - (uint32_t)sums[lo], (uint32_t)sums[a.n + 1 + lo]);
     r.entry = lo;
     r.first = (uint32_t)before[lo];
     return r;
@@ -232,7 +245,7 @@ __device__ inline KvShare kv_planned_share(const KvAttend &a, uint32_t u) {
 struct KvWork {
     int32_t entry, slot, length, begin, from, to;
     uint32_t steps;    // of the entry
-    bool whole, last;  // all of the entry; the share ends with it
+    bool whole, begins, last;  // all of the entry; its first part; the share ends with it
 };
 
 // One workgroup: an equal share of the batch's tokens, mostly a part of one entry's,
@@ -273,7 +286,7 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
     if (unit >= a.units) return;  // the grid is in eights
     // Without a.where, and always in a workgroup of many waves, a share is an entry.
     const bool shares = W == kKvWaves && a.where;
-    KvShare w{0, 1, 1, 0, 0, unit};
+    KvShare w{0, 1, 1, 0, 0, unit, 0};
     if (shares) {
         if (a.plan) w = kv_planned_share(a, (uint32_t)unit);
         else w = a.n <= 64    ? kv_find_share<1>(a, (uint32_t)unit)
@@ -283,6 +296,7 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
         w.end = (uint32_t)uniform((int)w.end);
         w.first = (uint32_t)uniform((int)w.first);
         w.entry = uniform(w.entry);
+        w.number = (uint32_t)uniform((int)w.number);
         if (w.entry < 0) return;
     }
     const uint32_t share_begin = w.begin, share_end = w.end;
@@ -330,12 +344,13 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
         x.steps = shares ? kv_steps(x.length - tile0) : 1;
         const KvPart part = shares ? kv_part(share_begin, share_end, first, x.steps) : KvPart{0, 1, true};
         x.whole = part.whole;
+        x.begins = part.from == 0;
         x.last = !shares || first + part.to >= share_end;
         x.from = tile0 + (int32_t)part.from * kKvStep;
         x.to = part.to == x.steps ? x.length : tile0 + (int32_t)part.to * kKvStep;
-        if (part.from == 0 && head == 0 && rg == 0 && threadIdx.x == 0) {
+        if (x.begins && head == 0 && rg == 0 && threadIdx.x == 0) {
             if (shares) {
-                a.where[2 * (int64_t)i] = unit + i;
+                a.where[2 * (int64_t)i] = (int32_t)kv_part_at(w.number, true);
                 a.where[2 * (int64_t)i + 1] = (int32_t)kv_parts(w.index, w.size, first, x.steps);
             }
             if (!known && slot != -1) atomicAdd(c.skipped, 1ull);
@@ -621,7 +636,7 @@ __global__ void __launch_bounds__(64 * W, kv_resident(E4M3, D, R, W)) kv_attend_
                         u32x4{IO::pack(u[0] * unit_v, v[0] * unit_v), IO::pack(u[1] * unit_v, v[1] * unit_v),
                               IO::pack(u[2] * unit_v, v[2] * unit_v), IO::pack(u[3] * unit_v, v[3] * unit_v)};
                 } else {
-                    const int64_t to_row = (int64_t)(unit + done.entry) * a.q_heads + at;
+                    const int64_t to_row = (int64_t)kv_part_at(w.number, done.begins) * a.q_heads + at;
                     if (j == 0 && g == 0) *(float2 *)(a.part_ml + 2 * to_row) = make_float2(most, sum);
                     float *dst = a.part_o + to_row * D + 32 * j + 8 * g;
                     *(f32x4 *)dst = f32x4{u[0], v[0], u[1], v[1]};
@@ -664,7 +679,7 @@ __global__ void __launch_bounds__(kv_join_threads(D, MANY)) kv_join_kernel(KvAtt
 #pragma unroll
             for (int i = 0; i < UP; ++i) {
                 const int32_t k = k0 + i * TEAMS;
-                const int64_t at = (int64_t)(first + (k < parts ? k : k0)) * a.q_heads + row;
+                const int64_t at = (int64_t)kv_part_next((uint32_t)first, (uint32_t)(k < parts ? k : k0)) * a.q_heads + row;
                 ml[i] = *(const float2 *)(a.part_ml + 2 * at);
                 po[i] = *(const f32x4 *)(a.part_o + at * D + 4 * col);
                 if (k >= parts) ml[i] = make_float2(-INFINITY, 0.f);

@@ -108,6 +108,20 @@ PR_KV_FN KvPart kv_part(uint32_t begin, uint32_t end, uint32_t first, uint32_t s
     p.whole = p.from == 0 && p.to == steps;
     return p;
 }
+// Where parts of sequences that have several are kept until they are joined.  A share has a
+// number: its own where shares go on from sequence to sequence (it then has two such parts
+// at most, one that begins its sequence and one that does not), else that among the shares of
+// sequences that have several.  `fill` shares of `size` steps or more are all the steps, so
+// of the latter there are less than 2 fill (a sequence with x > 1 times the steps of a share
+// has less than x + 1 < 2 x).
+PR_KV_FN uint32_t kv_part_at(uint32_t number, bool begins) { return 2 * number - !begins; }
+// ... and part k of a sequence whose first one is kept at `first`.
+PR_KV_FN uint32_t kv_part_next(uint32_t first, uint32_t k) { return first + (k ? 2 * k - 1 : 0); }
+PR_KV_FN int64_t kv_parts_kept(int64_t n, int64_t units, const KvSplit &s) {
+    const int64_t numbers = n < s.fill ? s.fill : 2 * (int64_t)s.fill;
+    return 2 * (numbers < units ? numbers : units);
+}
+
 // Parts of a sequence, the first of which is in share `share`.
 PR_KV_FN uint32_t kv_parts(uint32_t share, uint32_t c, uint32_t first, uint32_t steps) {
     return (first + steps - 1) / c - share + 1;

@@ -736,7 +736,12 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_plan_kernel(KvAttend a) {
     const uint32_t total = sums(a.plan, steps);
     if (!kv_keeps(total, a.n, a.split)) return;
     const uint32_t size = kv_share(total, a.split);
-    sums(a.plan + a.n + 1, [&](int64_t i) { return (steps(i) + size - 1) / size; });
+    auto shares = [&](int64_t i) { return (steps(i) + size - 1) / size; };
+    sums(a.plan + a.n + 1, shares);
+    sums(a.plan + 2 * (a.n + 1), [&](int64_t i) {
+        const uint32_t n = shares(i);
+        return n > 1 ? n : 0;
+    });
 }
 
 }  // namespace pr

@@ -222,9 +222,9 @@ int64_t attend_parts(const pr_kv *c, int64_t n, int32_t q_heads, int32_t window,
     a->part_ml = a->part_o = nullptr;
     if (!split) return 0;
     Parts p(work);
-    const int64_t parts = units + n;  // a share that goes on to the next sequence has two
+    const int64_t parts = pr::kv_parts_kept(n, units, a->split);
     a->where = p.take<int32_t>(2 * n);
-    a->plan = n > pr::kKvScan ? p.take<int32_t>(2 * n + 2) : nullptr;
+    a->plan = n > pr::kKvScan ? p.take<int32_t>(3 * n + 3) : nullptr;
     a->part_ml = p.take<float>(parts * q_heads * 2);
     a->part_o = p.take<float>(parts * q_heads * c->head_dim);
     return p.bytes;
