@@ -164,8 +164,12 @@ int64_t extend_parts(const pr_kv *c, int64_t n, int64_t rows, void *work, pr::Kv
     return p.bytes;
 }
 
-// A fork or trim whose tables have this many pages changes them in a second launch,
-// if its grid can be had.
+// A fork or trim whose tables have kKvShared pages changes them in a second launch, if its
+// grid can be had.  What sequences hold is not known here.  A fork and a trim, in one launch
+// each and in two: 256 entries with all of 513 scattered pages 80 and 15 us, with 64 of
+// them 15 and 13; 16 entries with 8,193 34 and 12, with 64 6 and 11.  Batches of less than
+// 16 have one launch, as room for so many pages each is mostly not used: 2 entries with 64
+// of 65,537 pages 6 and 13 us (but with all of them 236 and 18).
 dim3 column_grid(const pr_kv *c, int64_t n) {
     return dim3((unsigned)((c->slot_pages + 63) / 64), (unsigned)((n + pr::kKvSharedEntries - 1) / pr::kKvSharedEntries));
 }
