@@ -139,10 +139,6 @@ class KVCache:
             raise ValueError("stream must be of the cache's device")
         return _stream_ptr(stream, self.device)
 
-    def _layer(self, layer: int) -> int:
-        """The layer, or -1 for what is none (ctypes would cut it to 32 bits)."""
-        return layer if 0 <= layer < self.layers else -1
-
     def _ints(self, t, dtype, name, count=None) -> int:
         """Checks a vector of integers; its length."""
         _dev(t, dtype, name)
@@ -212,7 +208,8 @@ class KVCache:
         _, v_stride, v_io = self._rows(v, "v", rows, self.kv_heads)
         if io != v_io:
             raise TypeError("k and v must have one dtype")
-        s = self._lib.pr_kv_write(self._ref, self._layer(layer), place.data_ptr() or None, k.data_ptr() or None, k_stride,
+        layer = layer if 0 <= layer < self.layers else -1  # ctypes would cut it to 32 bits
+        s = self._lib.pr_kv_write(self._ref, layer, place.data_ptr() or None, k.data_ptr() or None, k_stride,
                                   v.data_ptr() or None, v_stride, rows, io, self._st(stream))
         if s != PR_OK:
             _check(s)
@@ -240,8 +237,9 @@ class KVCache:
                 raise ValueError("lse must be [n, heads] on the cache's device")
             self._no_derivative(lse, "lse")
         work, at, size = self._work(PR_KV_WORK_ATTEND, n, heads, stream)
-        s = self._lib.pr_kv_attend(self._ref, self._layer(layer), slots.data_ptr() or None, n, q.data_ptr() or None, stride,
-                                   heads, io, self._scale if scale is None else scale, min(max(window, -1), 0x7fffffff),
+        layer, window = layer if 0 <= layer < self.layers else -1, min(max(window, -1), 0x7fffffff)
+        s = self._lib.pr_kv_attend(self._ref, layer, slots.data_ptr() or None, n, q.data_ptr() or None, stride,
+                                   heads, io, self._scale if scale is None else scale, window,
                                    out.data_ptr() or None, lse.data_ptr() or None if lse is not None else None,
                                    at, size, st)
         if s != PR_OK:
