@@ -96,3 +96,26 @@ def test_attend_no_weight_beside_values_that_are_not_finite(kind):
         c.k[:, :, :, 0, :, 3] = 0  # all weights the same: each dimension is what its values make it
         out = c.attend(0, _ints([0, 1]), q, 1.0, lse=lse)
         assert not out[0, :, [5, 9, 60]].isfinite().any() and (out[:, :, [0, 4, 6, 63]] == 1).all()
+
+
+@pytest.mark.parametrize("kind,io", [("fp16", "fp16"), ("e4m3", "fp16")])
+def test_attend_numbers_below_the_normal_ones(kind, io):
+    """Subnormal half keys with large queries, and subnormal queries with large keys, make scores like any others."""
+    import torch
+    announce(f"attend with subnormal numbers, {kind}")
+    lengths, dim = [300, 20], 64
+    for small_keys in (True, False):
+        if small_keys and kind == "e4m3":
+            continue  # its smallest number is a normal half number
+        c = _cache(1, 2, dim, 16, 25, 2, 20, kind)
+        place = c.extend(_ints([0, 1]), _offsets(lengths), sum(lengths))
+        g = torch.Generator(device=device()).manual_seed(1)
+        k, v = (torch.empty((sum(lengths), 2, dim), device=device()).normal_(generator=g) for _ in "kv")
+        q = torch.empty((2, 4, dim), device=device()).normal_(generator=g)
+        k, q = (k * 2.0 ** -17, q * 2.0 ** 12) if small_keys else (k * 2.0 ** 6, q * 2.0 ** -17)
+        q = q.to(_types()[io])
+        c.write(0, place, k.to(_types()[io]), v.to(_types()[io]))
+        scale = 2.0 ** 4 if small_keys else 2.0 ** 10
+        lse = torch.empty((2, 4), device=device())
+        out = c.attend(0, _ints([0, 1]), q, scale, lse=lse)
+        _check_attend(c, 0, [0, 1], q, scale, 0, out, lse)
