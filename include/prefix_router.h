@@ -478,7 +478,8 @@ typedef struct {
     float k_scale;       /* PR_KV_E4M3: finite and positive; else 1 */
     float v_scale;
     void *k, *v;         /* 16-byte aligned */
-    int64_t k_layer, k_page, v_layer, v_page; /* strides in elements, of a multiple of 16 bytes */
+    int64_t k_layer, k_page, v_layer, v_page; /* strides in elements, of a multiple of 16 bytes, in any order
+                                                 in which no two pages overlap; all within 2^60 elements */
     int32_t *table;       /* [num_slots][slot_pages], -1 past a sequence's pages */
     int32_t *lengths;     /* [num_slots] */
     int32_t *refs;        /* [num_pages]: sequences that hold the page */
