@@ -523,7 +523,8 @@ pr_status pr_kv_extend(const pr_kv *c, const int32_t *slots, const int64_t *offs
 
 /*
  * Write keys and values of new tokens in one layer: row r (kv_heads * head_dim
- * numbers at k_rows + r * k_stride, v_rows + r * v_stride; strides in elements)
+ * numbers at k_rows + r * k_stride, v_rows + r * v_stride; strides in elements, so
+ * that rows do not overlap)
  * goes to place[r] (pr_kv_extend's).  io is the rows' type, PR_KV_BF16 or
  * PR_KV_F16: the cache's own, or either for a PR_KV_E4M3 cache, which takes the
  * nearest of its values to number / scale, ties to even, +-448 past its range,
@@ -541,7 +542,8 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  *   s_t = scale * q . k_t,  out = sum_t exp(s_t) v_t / sum_t exp(s_t),
  *   lse = log sum_t exp(s_t)
  * over its tokens t, the last `window` ones if window > 0.
- *   q    io (the cache's type; either 16-bit one for PR_KV_E4M3), 16-bit rows;
+ *   q    io (the cache's type; either 16-bit one for PR_KV_E4M3), rows that do
+ *        not overlap;
  *   out  io [n][q_heads][head_dim];
  *   lse  float [n][q_heads], or NULL.
  * A sequence without tokens, padding and a slot out of range (the latter
@@ -551,7 +553,8 @@ pr_status pr_kv_write(const pr_kv *c, int32_t layer, const int32_t *place, const
  * weight of 0, any other a NaN), and a dimension that is not finite from a
  * value.  A row all of whose weights are 0 is one without tokens.  Sums and
  * maxima are kept in 32 bits (values up to 2^88 cannot overflow them), and each
- * weight to 2^-17 of itself, however small it is beside the largest.
+ * weight to 2^-17 of itself, however small it is beside the largest (below
+ * 2^-126 of it, it is 0).
  * scale and scale * k_scale have to be finite.
  * q_heads: a multiple of kv_heads.  The same slot may occur more than once.
  * out must not overlap q (from its first to its last number).
